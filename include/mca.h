@@ -219,7 +219,9 @@ int mca_abi_version(void);
 
 /* sizeof of the ABI structs, so bindings can check their mirrors:
  * which = 0 mca_net_desc, 1 mca_cand, 2 mca_data, 3 mca_stats, 4 mca_trace,
- * 5 mca_timing, 6 mca_channel; 0 for any other value. */
+ * 5 mca_timing, 6 mca_channel, and of mca_lm.h 7 mca_cache_append_args,
+ * 8 mca_tree_attention_args, 9 mca_token_logprobs_args,
+ * 10 mca_token_logprobs_grad_args, 11 mca_extend_args; 0 for any other value. */
 size_t mca_struct_size(int32_t which);
 
 /* Device workspace bytes for a net, n_samples and at most k_max candidates per

@@ -24,6 +24,9 @@ Contents (each function cites the passage of the paper it follows):
 * ``normmlp``    fp64 deep MLPs of Sec. 2.1: biases, normalized hidden fields
                  and the layer-sticky proposal schedule.
 * ``transformer`` fp64 forward pass and loss of the pre-LN causal decoder.
+* ``lm``         the operators that answer with a trained language model:
+                 block tables, attention of drafted tokens over a paged cache,
+                 token log probabilities and their gradient.
 * ``mca``        the selection loop (Eq. 1, Eq. 5, Eq. 6, and the Metropolis
                  rule of Eq. 7 as a per-candidate threshold) over K candidates
                  per step in stream order, with pruning moves first and

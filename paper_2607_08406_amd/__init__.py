@@ -3,9 +3,11 @@ mutation-selection method (MCA): single-parameter mutation, incremental loss
 evaluation from cached local fields, greedy accept or roll back.
 
 The computation lives in the HIP library ``libmca.so`` (C ABI in
-``include/mca.h``); ``paper_2607_08406_amd.mca`` is its ctypes binding.
+``include/mca.h``); ``paper_2607_08406_amd.mca`` is its ctypes binding, and
+``paper_2607_08406_amd.lm`` that of the operators that answer with a trained
+language model (``include/mca_lm.h``).
 """
-from . import mca  # noqa: F401
+from . import lm, mca  # noqa: F401
 from .mca import Context, MCAError, TransformerContext, mlp_desc, transformer_desc  # noqa: F401
 
-__all__ = ["mca", "Context", "MCAError", "TransformerContext", "mlp_desc", "transformer_desc"]
+__all__ = ["lm", "mca", "Context", "MCAError", "TransformerContext", "mlp_desc", "transformer_desc"]

@@ -23,6 +23,7 @@
 #include "channel_kernels.hpp"
 #include "norm_kernels.hpp"
 #include "split_mma.hpp"
+#include "lm_kernels.hpp"
 #include "tf_kernels.hpp"
 
 using mca::Aux;
@@ -534,6 +535,14 @@ int device_fail(mca_ctx* ctx, hipError_t e, const char* what) {
     if ((ctx) == nullptr) return fail(nullptr, MCA_EINVAL, "ctx is NULL"); \
     if ((ctx)->poisoned) return fail(ctx, MCA_EPOISONED, "context poisoned by an earlier device error: " + (ctx)->err); \
   } while (0)
+
+// Sizes of an mca_extend call.
+int check_extend(mca_ctx* ctx, const mca_extend_args& x) {
+  if (!ctx->tf) return fail(ctx, MCA_EINVAL, "mca_extend takes a Transformer context");
+  int code;
+  const char* msg = mca::lm_check_attention(mca::tf_extend_attention(ctx->tfh, x), &code);
+  return msg == nullptr ? MCA_OK : fail(ctx, code, msg);
+}
 
 // Waits for a step loop's stream by polling it for up to a millisecond, then
 // blocks: after a short idle a blocking wait sleeps, and waking it costs tens of
@@ -1081,6 +1090,13 @@ int tf_init(mca_ctx** out, const mca_net_desc* net, const float* const* params, 
 
 }  // namespace
 
+namespace mca {
+
+int lm_fail(int code, const char* msg) { return fail(nullptr, code, msg); }
+int lm_device_fail(hipError_t e, const char* what) { return device_fail(nullptr, e, what); }
+
+}  // namespace mca
+
 extern "C" {
 
 int mca_abi_version(void) { return MCA_ABI_VERSION; }
@@ -1094,6 +1110,11 @@ size_t mca_struct_size(int32_t which) {
     case 4: return sizeof(mca_trace);
     case 5: return sizeof(mca_timing);
     case 6: return sizeof(mca_channel);
+    case 7: return sizeof(mca_cache_append_args);
+    case 8: return sizeof(mca_tree_attention_args);
+    case 9: return sizeof(mca_token_logprobs_args);
+    case 10: return sizeof(mca_token_logprobs_grad_args);
+    case 11: return sizeof(mca_extend_args);
     default: return 0;
   }
 }
@@ -1681,6 +1702,39 @@ int mca_get_sample_losses(mca_ctx* ctx, float* out_host) {
   }
   MCA_HIP(ctx, hipMemcpyAsync(out_host, ctx->net.ell, (size_t)ctx->net.N * sizeof(float), hipMemcpyDeviceToHost, ctx->stream));
   MCA_HIP(ctx, hipStreamSynchronize(ctx->stream));
+  return MCA_OK;
+}
+
+int mca_extend_plan(mca_ctx* ctx, const mca_extend_args* args, size_t* workspace_bytes) {
+  MCA_LIVE(ctx);
+  if (args == nullptr || workspace_bytes == nullptr) return fail(ctx, MCA_EINVAL, "args or workspace_bytes is NULL");
+  const int rc = check_extend(ctx, *args);
+  if (rc == MCA_OK) *workspace_bytes = mca::tf_extend_bytes(ctx->tfh, *args);
+  return rc;
+}
+
+int mca_extend(mca_ctx* ctx, const mca_extend_args* args) {
+  MCA_LIVE(ctx);
+  if (args == nullptr) return fail(ctx, MCA_EINVAL, "args is NULL");
+  const mca_extend_args& x = *args;
+  const int rc = check_extend(ctx, x);
+  if (rc != MCA_OK) return rc;
+  if (x.table_stride < x.max_blocks || x.logits_row < ctx->tfh.V || x.cache_layer < 0 || x.cache_layer % 4 != 0)
+    return fail(ctx, MCA_EINVAL, "table_stride must be at least max_blocks, logits_row the vocabulary, cache_layer a multiple of 4");
+  if (x.n_req == 0 || x.n_rows == 0) return MCA_OK;
+  if (!x.tokens || !x.parents || !x.offsets || !x.lengths || (!x.table && x.max_blocks > 0) || !x.k_cache || !x.v_cache ||
+      !x.qkv || !x.logits)
+    return fail(ctx, MCA_EINVAL, "an array is NULL");
+  for (const void* p : {(const void*)x.k_cache, (const void*)x.v_cache, (const void*)x.qkv})
+    if ((uintptr_t)p % 16 != 0) return fail(ctx, MCA_EINVAL, "the caches and qkv must be 16-byte aligned");
+  for (const void* p : {(const void*)x.tokens, (const void*)x.parents, (const void*)x.offsets, (const void*)x.lengths,
+                        (const void*)x.table, (const void*)x.logits})
+    if ((uintptr_t)p % 4 != 0) return fail(ctx, MCA_EINVAL, "an array is not aligned to its elements");
+  if (x.workspace == nullptr || (uintptr_t)x.workspace % kAlign != 0)
+    return fail(ctx, MCA_EINVAL, "workspace must be a 256-byte aligned array");
+  if (x.workspace_bytes < mca::tf_extend_bytes(ctx->tfh, x))
+    return fail(ctx, MCA_ENOSPACE, "workspace smaller than mca_extend_plan()");
+  MCA_HIP(ctx, mca::tf_launch_extend(ctx->tfd, ctx->tfh, x, ctx->stream));
   return MCA_OK;
 }
 

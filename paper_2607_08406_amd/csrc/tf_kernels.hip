@@ -29,6 +29,8 @@
 // (v_mfma_f32_16x16x4f32), its softmax, GELU and the loss the vector units.
 #include <algorithm>
 
+#include "lm_device.hpp"
+#include "lm_kernels.hpp"
 #include "split_mma.hpp"
 #include "tf_kernels.hpp"
 
@@ -1048,28 +1050,21 @@ hipError_t tf_launch_prepare(const TfDev* tf, mca_cand* cands, int K, Aux* aux,
 }
 
 
-hipError_t tf_launch_eval(const TfDev* tf, const TfDev& h, const mca_cand* cands,
-                          const Aux* aux, int K, bool identity, float* partial, int nblk,
-                          hipStream_t s) {
-  const int ncand = identity ? 1 : K;
-  const unsigned rows = identity ? 1u : (unsigned)(K + 1);  // + the pending recomputation
-  const int64_t N = h.N;
+// The stages of every active slot over N positions, from block 1's first
+// LayerNorm to the logits and losses: dev(stage) is the description that a
+// stage's kernels read, attention(stage) launches a block's attention.
+template <class Dev, class Attn>
+static void launch_stages(const TfDev& h, int64_t N, unsigned rows, int ncand, const mca_cand* cands, const Aux* aux,
+                          hipStream_t s, Dev dev, Attn attention) {
   const unsigned mt = (unsigned)((N + kGemmRows - 1) / kGemmRows);
   auto tiles = [](int64_t n, int w) { return (unsigned)((n + w - 1) / w); };
-  hipLaunchKernelGGL(k_tf_prep,
-                     dim3((unsigned)((h.copy_stride + kCopyChunk - 1) / kCopyChunk), rows),
-                     dim3(kCopyThreads), 0, s, tf, cands, aux, identity ? kPrepIdentity : kPrepEval,
-                     ncand);
-  hipLaunchKernelGGL(k_tf_embed,
-                     dim3((unsigned)((N * h.D + kCopyThreads * kEmbedPer - 1) / (kCopyThreads * kEmbedPer)), rows),
-                     dim3(kCopyThreads), 0, s, tf, ncand);
   const dim3 srow((unsigned)((N + (kRowThreads / 64) * 4 * kStatSteps - 1) / ((kRowThreads / 64) * 4 * kStatSteps)), rows);
   const bool wide = h.D > 128;  // row pairs per lane of the 16-lane layout: 4 or 8
   auto stats = [&](int stage, int which) {
     if (wide)
-      hipLaunchKernelGGL(k_tf_stats<8>, srow, dim3(kRowThreads), 0, s, tf, cands, aux, stage, which, ncand);
+      hipLaunchKernelGGL(k_tf_stats<8>, srow, dim3(kRowThreads), 0, s, dev(stage), cands, aux, stage, which, ncand);
     else
-      hipLaunchKernelGGL(k_tf_stats<4>, srow, dim3(kRowThreads), 0, s, tf, cands, aux, stage, which, ncand);
+      hipLaunchKernelGGL(k_tf_stats<4>, srow, dim3(kRowThreads), 0, s, dev(stage), cands, aux, stage, which, ncand);
   };
   // 128-column tiles, or 64-column ones where those leave fewer columns unused or
   // the wide ones would not give every CU two blocks (a block's time is a chain of
@@ -1078,15 +1073,15 @@ hipError_t tf_launch_eval(const TfDev* tf, const TfDev& h, const mca_cand* cands
   // 256, 1513 us wide, 1605 narrow).  Every output's sum is the same bits in both.
   auto gemm = [&](auto wide_tile, auto narrow_tile, int stage, int nout, int role) {
     if (tiles(nout, 128) * 2 == tiles(nout, 64) && (int64_t)mt * tiles(nout, 128) * rows >= 512)
-      hipLaunchKernelGGL(wide_tile, dim3(mt, tiles(nout, 128), rows), dim3(kGemmThreads), 0, s, tf, stage, role, ncand);
+      hipLaunchKernelGGL(wide_tile, dim3(mt, tiles(nout, 128), rows), dim3(kGemmThreads), 0, s, dev(stage), stage, role, ncand);
     else
-      hipLaunchKernelGGL(narrow_tile, dim3(mt, tiles(nout, 64), rows), dim3(kGemmThreads), 0, s, tf, stage, role, ncand);
+      hipLaunchKernelGGL(narrow_tile, dim3(mt, tiles(nout, 64), rows), dim3(kGemmThreads), 0, s, dev(stage), stage, role, ncand);
   };
   for (int b = 0; b < h.NB; ++b) {
     const int stage = b + 1;
     stats(stage, 0);
     gemm(k_tf_gemm<0, 4, 2>, k_tf_gemm<0, 2, 2>, stage, 3 * h.D, kGemmQKV);
-    hipLaunchKernelGGL(k_tf_attn, dim3((unsigned)(h.S * h.H), rows), dim3(256), 0, s, tf, stage, ncand);
+    attention(stage);
     gemm(k_tf_gemm<2, 4, 2>, k_tf_gemm<2, 2, 2>, stage, h.D, kGemmO);
     stats(stage, 1);
     gemm(k_tf_gemm<1, 4, 2>, k_tf_gemm<1, 2, 2>, stage, h.M, kGemmFc);
@@ -1095,13 +1090,31 @@ hipError_t tf_launch_eval(const TfDev* tf, const TfDev& h, const mca_cand* cands
   stats(h.NB + 1, 2);
   // the output layer: one column tile over the vocabulary (80 or 128 wide)
   if (h.V <= 80)
-    hipLaunchKernelGGL((k_tf_gemm<3, 5, 1>), dim3(mt, 1, rows), dim3(kGemmThreads), 0, s, tf, h.NB + 1,
+    hipLaunchKernelGGL((k_tf_gemm<3, 5, 1>), dim3(mt, 1, rows), dim3(kGemmThreads), 0, s, dev(h.NB + 1), h.NB + 1,
                        (int)kGemmOut, ncand);
   else
-    hipLaunchKernelGGL((k_tf_gemm<3, 8, 1>), dim3(mt, 1, rows), dim3(kGemmThreads), 0, s, tf, h.NB + 1,
+    hipLaunchKernelGGL((k_tf_gemm<3, 8, 1>), dim3(mt, 1, rows), dim3(kGemmThreads), 0, s, dev(h.NB + 1), h.NB + 1,
                        (int)kGemmOut, ncand);
+}
+
+hipError_t tf_launch_eval(const TfDev* tf, const TfDev& h, const mca_cand* cands,
+                          const Aux* aux, int K, bool identity, float* partial, int nblk,
+                          hipStream_t s) {
+  const int ncand = identity ? 1 : K;
+  const unsigned rows = identity ? 1u : (unsigned)(K + 1);  // + the pending recomputation
+  const int64_t N = h.N;
+  hipLaunchKernelGGL(k_tf_prep,
+                     dim3((unsigned)((h.copy_stride + kCopyChunk - 1) / kCopyChunk), rows),
+                     dim3(kCopyThreads), 0, s, tf, cands, aux, identity ? kPrepIdentity : kPrepEval,
+                     ncand);
+  hipLaunchKernelGGL(k_tf_embed,
+                     dim3((unsigned)((N * h.D + kCopyThreads * kEmbedPer - 1) / (kCopyThreads * kEmbedPer)), rows),
+                     dim3(kCopyThreads), 0, s, tf, ncand);
+  launch_stages(h, N, rows, ncand, cands, aux, s, [&](int) { return tf; }, [&](int stage) {
+    hipLaunchKernelGGL(k_tf_attn, dim3((unsigned)(h.S * h.H), rows), dim3(256), 0, s, tf, stage, ncand);
+  });
   if (!identity && K > 0) {
-    if (wide)
+    if (h.D > 128)
       hipLaunchKernelGGL(k_tf_dl<8>, dim3((unsigned)nblk, (unsigned)K), dim3(kLossThreads), 0, s, tf,
                          cands, aux, partial, nblk);
     else
@@ -1123,6 +1136,188 @@ hipError_t tf_launch_commit(const TfDev* tf, const TfDev& h, const mca_cand* can
     hipLaunchKernelGGL(k_tf_loss_total, dim3(1), dim3(64), 0, s, tf, bsum, nb, st);
   }
   return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// the committed net on drafted nodes (mca_extend)
+// ---------------------------------------------------------------------------
+
+namespace {
+
+// Workspace of mca_extend.
+struct ExtLayout {
+  size_t dev, table, flags, sx, sh, satt, sfc, slog, sell, sst, tgt, attn;
+  size_t total;
+};
+ExtLayout ext_layout(const TfDev& h, int64_t n, size_t attn_bytes) {
+  ExtLayout lo;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off = (off + bytes + 255) / 256 * 256;
+    return at;
+  };
+  const size_t N = (size_t)n, D = (size_t)h.D, NB = (size_t)h.NB;
+  lo.dev = take(NB * sizeof(TfDev));
+  lo.table = take((size_t)h.n_tensors * sizeof(float*));
+  lo.flags = take(5 * 2 * sizeof(int32_t));
+  lo.sx = take((NB + 1) * N * D * sizeof(float));
+  lo.sh = take(NB * N * D * sizeof(float));
+  lo.satt = take(N * D * sizeof(float));
+  lo.sfc = take(N * (size_t)h.M * sizeof(float));
+  lo.slog = take(N * (size_t)h.V * sizeof(float));
+  lo.sell = take(N * sizeof(float));
+  lo.sst = take(N * sizeof(float2));
+  lo.tgt = take(N * sizeof(int32_t));
+  lo.attn = take(attn_bytes);
+  lo.total = off;
+  return lo;
+}
+
+}  // namespace
+
+// The descriptions of the call's stages, one a block (they differ in where the
+// projections go): the context's own, with the call's rows as the positions of
+// slot 0, which runs every stage with the committed tensors.
+__global__ __launch_bounds__(256) void k_tf_ext_setup(const TfDev* tf, char* ws, ExtLayout lo, int64_t N, float* qkv) {
+  static_assert(sizeof(TfDev) % 4 == 0, "copied in words");
+  const int nt = tf->n_tensors, NB = tf->NB;
+  TfDev* dev = (TfDev*)(ws + lo.dev);
+  if (blockIdx.x > 0) {
+    const int64_t n = (int64_t)(blockIdx.x - 1) * blockDim.x + threadIdx.x;
+    if (n < N) ((int32_t*)(ws + lo.tgt))[n] = 0;
+    return;
+  }
+  constexpr int kWords = (int)(sizeof(TfDev) / 4);
+  for (int e = threadIdx.x; e < NB * kWords; e += blockDim.x) ((uint32_t*)dev)[e] = ((const uint32_t*)tf)[e % kWords];
+  float** table = (float**)(ws + lo.table);
+  for (int t = threadIdx.x; t < nt; t += blockDim.x) table[t] = tf->param[t];
+  int32_t* flags = (int32_t*)(ws + lo.flags);  // start, run, xin, half, kind of slots 0 and 1
+  if (threadIdx.x < 10) flags[threadIdx.x] = (threadIdx.x & 1) && threadIdx.x < 6 ? NB + 2 : 0;
+  __syncthreads();
+  if (threadIdx.x < NB) {
+    TfDev& d = dev[threadIdx.x];
+    d.N = N;
+    d.sx = (float*)(ws + lo.sx);
+    d.sh = (float*)(ws + lo.sh);
+    d.satt = (float*)(ws + lo.satt);
+    d.sfc = (float*)(ws + lo.sfc);
+    d.slog = (float*)(ws + lo.slog);
+    d.sell = (float*)(ws + lo.sell);
+    d.sst = (float2*)(ws + lo.sst);
+    d.tgt = (const int32_t*)(ws + lo.tgt);
+    d.table = table;
+    d.start = flags;
+    d.run = flags + 2;
+    d.xin = flags + 4;
+    d.half = flags + 6;
+    d.kind = flags + 8;
+    d.kr = 1;
+    d.sqkv = qkv + threadIdx.x * 3 * N * d.D;
+  }
+}
+
+// x_0 of a request's nodes: a node's position is the request's cached tokens
+// plus its depth, found by pointer doubling.  NaN for a token outside the
+// vocabulary or a position outside the context.
+__global__ __launch_bounds__(kCopyThreads) void k_tf_ext_embed(const TfDev* tf, mca_tree_attention_args a,
+                                                               const int32_t* tokens, float* x0) {
+  __shared__ int s_up[2][MCA_MAX_NODES], s_depth[2][MCA_MAX_NODES];
+  const int r = blockIdx.x, tid = threadIdx.x, D = tf->D;
+  int first, n;
+  if (!rows_of(a, r, &first, &n)) return;
+  if (tid < n) {
+    const int up = a.parents[first + tid];
+    s_up[0][tid] = up >= 0 && up < tid ? up : -1;
+    s_depth[0][tid] = s_up[0][tid] >= 0 ? 1 : 0;
+  }
+  int from = 0;
+  for (int d = 1; d < n; d <<= 1) {
+    __syncthreads();
+    if (tid < n) {
+      const int up = s_up[from][tid];
+      s_up[from ^ 1][tid] = up >= 0 ? s_up[from][up] : -1;
+      s_depth[from ^ 1][tid] = s_depth[from][tid] + (up >= 0 ? s_depth[from][up] : 0);
+    }
+    from ^= 1;
+  }
+  __syncthreads();
+  const int len = cached_of(a, r);
+  const float* te = tf->param[0];
+  const float* pe = tf->param[1];
+  for (int e = tid; e < n * D; e += kCopyThreads) {
+    const int i = e / D, c = e - i * D, tok = tokens[first + i], pos = len + s_depth[from][i];
+    const bool ok = tok >= 0 && tok < tf->V && pos < tf->T;
+    x0[(int64_t)(first + i) * D + c] = ok ? te[(int64_t)tok * D + c] + pe[(int64_t)pos * D + c] : __builtin_nanf("");
+  }
+}
+
+__global__ __launch_bounds__(kCopyThreads) void k_tf_ext_logits(const TfDev* tf, mca_tree_attention_args a, const float* z,
+                                                                float* logits, int64_t logits_row) {
+  int first, n;
+  if (!rows_of(a, blockIdx.x, &first, &n)) return;
+  const int V = tf->V;
+  for (int e = threadIdx.x; e < n * V; e += kCopyThreads) {
+    const int i = e / V, c = e - i * V;
+    logits[(first + i) * logits_row + c] = z[(int64_t)(first + i) * V + c];
+  }
+}
+
+mca_tree_attention_args tf_extend_attention(const TfDev& h, const mca_extend_args& x) {
+  mca_tree_attention_args a{};
+  a.dtype = MCA_TYPE_F32;
+  a.n_req = x.n_req;
+  a.n_head = a.n_kv_head = h.H;
+  a.head_dim = kTfHeadDim;
+  a.block_size = x.block_size;
+  a.n_blocks = x.n_blocks;
+  a.max_blocks = x.max_blocks;
+  a.max_nodes = x.max_nodes;
+  a.max_len = x.max_len;
+  a.scale = 0.17677669529663687f;  // 1 / sqrt(32)
+  a.n_rows = x.n_rows;
+  a.table_stride = x.table_stride;
+  a.q_row = a.k_row = a.v_row = 3 * h.D;
+  a.out_row = h.D;
+  a.q_head = a.k_head = a.v_head = a.out_head = kTfHeadDim;
+  a.table = x.table;
+  a.lengths = x.lengths;
+  a.offsets = x.offsets;
+  a.parents = x.parents;
+  return a;
+}
+
+size_t tf_extend_bytes(const TfDev& h, const mca_extend_args& x) {
+  return ext_layout(h, x.n_rows, lm_attention_plan(tf_extend_attention(h, x)).bytes).total;
+}
+
+hipError_t tf_launch_extend(const TfDev* tf, const TfDev& h, const mca_extend_args& x, hipStream_t s) {
+  mca_tree_attention_args a = tf_extend_attention(h, x);
+  const AttnPlan plan = lm_attention_plan(a);
+  const int64_t N = x.n_rows;
+  const ExtLayout lo = ext_layout(h, N, plan.bytes);
+  char* ws = (char*)x.workspace;
+  TfDev* dev = (TfDev*)(ws + lo.dev);
+  a.out = ws + lo.satt;
+  a.workspace = ws + lo.attn;
+  a.workspace_bytes = plan.bytes;
+  hipLaunchKernelGGL(k_tf_ext_setup, dim3(1 + (unsigned)((N + 255) / 256)), dim3(256), 0, s, tf, ws, lo, N, x.qkv);
+  hipLaunchKernelGGL(k_tf_ext_embed, dim3((unsigned)x.n_req), dim3(kCopyThreads), 0, s, tf, a, x.tokens, (float*)(ws + lo.sx));
+  hipError_t e = hipSuccess;
+  launch_stages(h, N, 1, 1, nullptr, nullptr, s, [&](int stage) { return dev + (stage <= h.NB ? stage - 1 : 0); },
+                [&](int stage) {
+                  const int64_t b = stage - 1;
+                  a.q = x.qkv + b * 3 * N * h.D;
+                  a.k = (const float*)a.q + h.D;
+                  a.v = (const float*)a.q + 2 * h.D;
+                  a.k_cache = x.k_cache + b * x.cache_layer;
+                  a.v_cache = x.v_cache + b * x.cache_layer;
+                  const hipError_t ea = lm_launch_attention(a, plan, s);
+                  if (e == hipSuccess) e = ea;
+                });
+  hipLaunchKernelGGL(k_tf_ext_logits, dim3((unsigned)x.n_req), dim3(kCopyThreads), 0, s, tf, a, (const float*)(ws + lo.slog),
+                     x.logits, x.logits_row);
+  return e == hipSuccess ? hipGetLastError() : e;
 }
 
 }  // namespace mca

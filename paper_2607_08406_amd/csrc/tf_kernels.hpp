@@ -7,6 +7,7 @@
 
 #include "device_common.hpp"
 #include "mca.h"
+#include "mca_lm.h"
 
 namespace mca {
 
@@ -137,5 +138,12 @@ hipError_t tf_launch_commit(const TfDev* tf, const TfDev& h, const mca_cand* can
                             const Aux* aux, const double* dL, DevState* st, int k, bool fill,
                             double* bsum, hipStream_t s);
 int tf_loss_blocks(int64_t N);
+
+// mca_extend: the attention call of its blocks (sizes, strides and the arrays
+// of requests), its workspace, and the pass over the call's rows with the
+// committed tensors, on a description of its own that is made from tf.
+mca_tree_attention_args tf_extend_attention(const TfDev& h, const mca_extend_args& x);
+size_t tf_extend_bytes(const TfDev& h, const mca_extend_args& x);
+hipError_t tf_launch_extend(const TfDev* tf, const TfDev& h, const mca_extend_args& x, hipStream_t s);
 
 }  // namespace mca

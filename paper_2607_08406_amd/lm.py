@@ -1,0 +1,360 @@
+"""ctypes binding of the language-model operators (include/mca_lm.h): same names,
+argument marshalling only.
+
+Tensors pass as they are: their strides go to the library, and what it does not
+take is refused, not copied.  The work goes on the current stream of the tensors'
+device, and workspaces come from PyTorch's allocator on that stream unless one is
+given.  Nothing is synchronised.
+"""
+from __future__ import annotations
+
+import ctypes
+import math
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import mca
+from .mca import (MCA_EDEVICE, MCA_EINVAL, MCAError, _check, load_library, mca_cache_append_args, mca_extend_args,
+                  mca_token_logprobs_args, mca_token_logprobs_grad_args, mca_tree_attention_args)
+
+MCA_TYPE_F32, MCA_TYPE_BF16, MCA_TYPE_F16 = 0, 1, 2
+MCA_MAX_NODES, MCA_MAX_TOP, MCA_MAX_REQ = 128, 32, 65535
+MCA_TABLES_OK, MCA_TABLES_EXHAUSTED, MCA_TABLES_LENGTH, MCA_TABLES_SLOTS = 0, 1, 2, 3
+
+_TYPES = {torch.float32: MCA_TYPE_F32, torch.bfloat16: MCA_TYPE_BF16, torch.float16: MCA_TYPE_F16}
+
+
+def _refuse(msg: str):
+    raise MCAError(MCA_EINVAL, msg)
+
+
+def _type(t: torch.Tensor) -> int:
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        _refuse(f"{t.dtype} values: the operators take float32, bfloat16 and float16")
+    return code
+
+
+def _on(device, dtype, what, t, dim):
+    """t is a tensor of that device, type and number of dimensions, the last one contiguous."""
+    if t.device != device:
+        _refuse(f"{what} is on {t.device}, not {device}")
+    if t.dtype != dtype:
+        _refuse(f"{what} holds {t.dtype}, not {dtype}")
+    if t.dim() != dim:
+        _refuse(f"{what} has {t.dim()} dimensions, not {dim}")
+    if dim and t.stride(-1) != 1 and t.size(-1) > 1:
+        _refuse(f"{what} is not contiguous in its last dimension")
+
+
+def _flat(device, dtype, what, t, size):
+    _on(device, dtype, what, t, 1)
+    if t.numel() != size:
+        _refuse(f"{what} has {t.numel()} entries, not {size}")
+
+
+def _whole(device, dtype, what, t, shape):
+    _on(device, dtype, what, t, len(shape))
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        _refuse(f"{what} is not a contiguous tensor of shape {tuple(shape)}")
+
+
+def _gpu(t: torch.Tensor) -> torch.device:
+    if not t.is_cuda:
+        raise MCAError(MCA_EDEVICE, f"a tensor on {t.device}: the operators run only on the GPU")
+    return t.device
+
+
+def _stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _run(device, call, *args):
+    if torch.cuda.current_device() == device.index:
+        _check(call(*args, _stream(device)))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, _stream(device)))
+
+
+def _room(device, nbytes, workspace):
+    if workspace is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    _on(device, torch.uint8, "workspace", workspace, 1)
+    return workspace
+
+
+# ---------------------------------------------------------------------------
+# the cache
+# ---------------------------------------------------------------------------
+
+def mca_block_tables(old_len, new_len, table, free_list, block_size: int, offsets, slots, status):
+    """Update table [n_req, max_blocks] and free_list [n_blocks] for requests that go from old_len to
+    new_len [n_req] tokens; offsets [n_req + 1], slots [max_tokens] (int64) and status [4] are written."""
+    dev, i32 = _gpu(table), torch.int32
+    _on(dev, i32, "table", table, 2)
+    n = table.shape[0]
+    _flat(dev, i32, "old_len", old_len, n)
+    _flat(dev, i32, "new_len", new_len, n)
+    _on(dev, i32, "free_list", free_list, 1)
+    _flat(dev, i32, "offsets", offsets, n + 1)
+    _on(dev, torch.int64, "slots", slots, 1)
+    _flat(dev, i32, "status", status, 4)
+    _run(dev, load_library().mca_block_tables, old_len.data_ptr(), new_len.data_ptr(), n, block_size, table.data_ptr(),
+         table.stride(0) if n > 1 else table.shape[1], table.shape[1], free_list.data_ptr(), free_list.numel(),
+         offsets.data_ptr(), slots.data_ptr(), slots.numel(), status.data_ptr())
+
+
+def mca_cache_append(k, v, k_cache, v_cache, slots, rows=None):
+    """Row i (rows[i] with rows) of k and v [n_src, n_kv_head, head_dim] into slot slots[i] of the caches
+    [n_blocks, n_kv_head, block_size, head_dim]."""
+    dev, dt = _gpu(k_cache), k_cache.dtype
+    a = mca_cache_append_args()
+    a.dtype = _type(k_cache)
+    if k_cache.dim() != 4:
+        _refuse("k_cache has 4 dimensions")
+    _whole(dev, dt, "k_cache", k_cache, k_cache.shape)
+    _whole(dev, dt, "v_cache", v_cache, k_cache.shape)
+    _on(dev, dt, "k", k, 3)
+    _on(dev, dt, "v", v, 3)
+    a.n_blocks, a.n_kv_head, a.block_size, a.head_dim = k_cache.shape
+    if k.shape != v.shape or tuple(k.shape[1:]) != (a.n_kv_head, a.head_dim):
+        _refuse("k and v must be [n_src, n_kv_head, head_dim] like the caches' heads")
+    _on(dev, torch.int64, "slots", slots, 1)
+    a.n, a.n_src = slots.numel(), k.shape[0]
+    if rows is not None:
+        _flat(dev, torch.int32, "rows", rows, a.n)
+        a.rows = rows.data_ptr()
+    elif a.n != a.n_src:
+        _refuse("without rows, slots has an entry for each row of k")
+    a.k, a.v, a.k_cache, a.v_cache = k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr()
+    a.k_row, a.k_head, _ = k.stride()
+    a.v_row, a.v_head, _ = v.stride()
+    a.slots = slots.data_ptr()
+    _run(dev, load_library().mca_cache_append, ctypes.byref(a))
+
+
+# ---------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------
+
+def _attention_args(q, k, v, k_cache, v_cache, table, lengths, offsets, parents, max_nodes, max_len, scale, out, lse):
+    dev, dt, i32 = _gpu(q), q.dtype, torch.int32
+    a = mca_tree_attention_args()
+    a.dtype = _type(q)
+    _on(dev, dt, "q", q, 3)
+    _on(dev, dt, "k", k, 3)
+    _on(dev, dt, "v", v, 3)
+    if k_cache.dim() != 4:
+        _refuse("k_cache has 4 dimensions")
+    _whole(dev, dt, "k_cache", k_cache, k_cache.shape)
+    _whole(dev, dt, "v_cache", v_cache, k_cache.shape)
+    a.n_rows, a.n_head, a.head_dim = q.shape
+    a.n_blocks, a.n_kv_head, a.block_size, dim = k_cache.shape
+    if k.shape != v.shape or tuple(k.shape) != (a.n_rows, a.n_kv_head, a.head_dim) or dim != a.head_dim:
+        _refuse("q, k, v and the caches must agree in rows, heads and head_dim")
+    _on(dev, i32, "table", table, 2)
+    a.n_req, a.max_blocks = table.shape
+    _flat(dev, i32, "lengths", lengths, a.n_req)
+    _flat(dev, i32, "offsets", offsets, a.n_req + 1)
+    _flat(dev, i32, "parents", parents, a.n_rows)
+    _on(dev, dt, "out", out, 3)
+    if out.shape != q.shape:
+        _refuse("out must have q's shape")
+    if lse is not None:
+        _whole(dev, torch.float32, "lse", lse, q.shape[:2])
+        a.lse = lse.data_ptr()
+    a.max_nodes = max_nodes
+    a.max_len = a.max_blocks * a.block_size if max_len is None else max_len
+    a.scale = 1.0 / math.sqrt(a.head_dim) if scale is None else scale
+    a.table_stride = table.stride(0) if a.n_req > 1 else a.max_blocks
+    a.q, a.k, a.v, a.out = q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr()
+    a.q_row, a.q_head, _ = q.stride()
+    a.k_row, a.k_head, _ = k.stride()
+    a.v_row, a.v_head, _ = v.stride()
+    a.out_row, a.out_head, _ = out.stride()
+    a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
+    a.table, a.lengths = table.data_ptr(), lengths.data_ptr()
+    a.offsets, a.parents = offsets.data_ptr(), parents.data_ptr()
+    return dev, a
+
+
+def mca_tree_attention_plan(q, k_cache, n_req: int, max_blocks: int, max_nodes: int, max_len: Optional[int] = None) -> int:
+    """Workspace bytes of mca_tree_attention on tensors of these shapes."""
+    a = mca_tree_attention_args()
+    a.dtype = _type(q)
+    a.n_rows, a.n_head, a.head_dim = q.shape
+    a.n_blocks, a.n_kv_head, a.block_size, _ = k_cache.shape
+    a.n_req, a.max_blocks, a.max_nodes = n_req, max_blocks, max_nodes
+    a.max_len = max_blocks * a.block_size if max_len is None else max_len
+    return _plan(a, load_library().mca_tree_attention_plan)
+
+
+def _plan(a, call) -> int:
+    n = ctypes.c_size_t(0)
+    _check(call(ctypes.byref(a), ctypes.byref(n)))
+    return n.value
+
+
+def mca_tree_attention(q, k, v, k_cache, v_cache, table, lengths, offsets, parents, max_nodes: int,
+                       max_len: Optional[int] = None, scale: Optional[float] = None, out=None, lse=None,
+                       workspace=None):
+    """Attention of drafted nodes over the cache and their ancestors; returns (out, lse).
+
+    q [n_rows, n_head, head_dim], k and v [n_rows, n_kv_head, head_dim]; request r has rows offsets[r] ..
+    offsets[r + 1] - 1 and lengths[r] <= max_len cached tokens (default: what its table holds).  scale defaults to
+    1 / sqrt(head_dim).  Rows of a given out and lse behind the last request stay as they were; those of new ones
+    are zero.
+    """
+    if out is None:
+        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
+    dev, a = _attention_args(q, k, v, k_cache, v_cache, table, lengths, offsets, parents, max_nodes, max_len, scale,
+                             out, lse)
+    lib = load_library()
+    nbytes = _plan(a, lib.mca_tree_attention_plan)
+    if nbytes:
+        room = _room(dev, nbytes, workspace)
+        a.workspace, a.workspace_bytes = room.data_ptr(), room.numel()
+    _run(dev, lib.mca_tree_attention, ctypes.byref(a))
+    return out, lse
+
+
+# ---------------------------------------------------------------------------
+# log probabilities
+# ---------------------------------------------------------------------------
+
+class TokenLogprobs(NamedTuple):
+    logprob: torch.Tensor      # [n_rows] of the given tokens
+    entropy: torch.Tensor      # [n_rows]
+    lse: torch.Tensor          # [n_rows]
+    top_logprob: torch.Tensor  # [n_rows, n_top]
+    top_id: torch.Tensor       # [n_rows, n_top] int32
+
+
+def _logits(logits, tokens):
+    dev = _gpu(logits)
+    _on(dev, logits.dtype, "logits", logits, 2)
+    if tokens.dtype not in (torch.int32, torch.int64):
+        _refuse("tokens must be int32 or int64")
+    _flat(dev, tokens.dtype, "tokens", tokens, logits.shape[0])
+    return dev, logits.stride(0) if logits.shape[0] > 1 else logits.shape[1]
+
+
+def mca_token_logprobs_plan(logits, n_top: int = 0) -> int:
+    """Workspace bytes of mca_token_logprobs on logits of this shape."""
+    a = mca_token_logprobs_args()
+    a.dtype, a.n_top = _type(logits), n_top
+    a.n_rows, a.n_vocab = logits.shape
+    return _plan(a, load_library().mca_token_logprobs_plan)
+
+
+def mca_token_logprobs(logits, tokens, n_top: int = 0, workspace=None) -> TokenLogprobs:
+    """Log probabilities of tokens [n_rows] under logits [n_rows, n_vocab], entropies and the n_top alternatives."""
+    dev, row = _logits(logits, tokens)
+    a = mca_token_logprobs_args()
+    a.dtype, a.n_top, a.token_bytes = _type(logits), n_top, tokens.element_size()
+    n, a.n_vocab = logits.shape
+    a.n_rows, a.logits_row = n, row
+    lib = load_library()
+    nbytes = _plan(a, lib.mca_token_logprobs_plan)
+    f = torch.empty((3, n), dtype=torch.float32, device=dev)
+    top = torch.empty((n, n_top), dtype=torch.float32, device=dev)
+    ids = torch.empty((n, n_top), dtype=torch.int32, device=dev)
+    a.logits, a.tokens = logits.data_ptr(), tokens.data_ptr()
+    a.logprob, a.entropy, a.lse = f[0].data_ptr(), f[1].data_ptr(), f[2].data_ptr()
+    a.top_logprob, a.top_id = top.data_ptr(), ids.data_ptr()
+    if nbytes:
+        room = _room(dev, nbytes, workspace)
+        a.workspace, a.workspace_bytes = room.data_ptr(), room.numel()
+    _run(dev, lib.mca_token_logprobs, ctypes.byref(a))
+    return TokenLogprobs(f[0], f[1], f[2], top, ids)
+
+
+def mca_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, grad_entropy=None, out=None):
+    """Gradient with respect to the logits of sum grad_logprob * logprob + grad_entropy * entropy; out may be logits."""
+    dev, row = _logits(logits, tokens)
+    n, f32 = logits.shape[0], torch.float32
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    _on(dev, logits.dtype, "out", out, 2)
+    if out.shape != logits.shape:
+        _refuse("out must have the logits' shape")
+    a = mca_token_logprobs_grad_args()
+    a.dtype, a.token_bytes = _type(logits), tokens.element_size()
+    a.n_rows, a.n_vocab = logits.shape
+    a.logits_row, a.grad_row = row, out.stride(0) if n > 1 else out.shape[1]
+    a.logits, a.tokens, a.grad = logits.data_ptr(), tokens.data_ptr(), out.data_ptr()
+    _flat(dev, f32, "lse", lse, n)
+    a.lse = lse.data_ptr()
+    if grad_logprob is not None:
+        _flat(dev, f32, "grad_logprob", grad_logprob, n)
+        a.grad_logprob = grad_logprob.data_ptr()
+    if grad_entropy is not None:
+        _flat(dev, f32, "grad_entropy", grad_entropy, n)
+        _flat(dev, f32, "entropy", entropy, n)
+        a.grad_entropy, a.entropy = grad_entropy.data_ptr(), entropy.data_ptr()
+    _run(dev, load_library().mca_token_logprobs_grad, ctypes.byref(a))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# the committed net of a Transformer context
+# ---------------------------------------------------------------------------
+
+def _extend_args(dev, desc, tokens, parents, offsets, lengths, table, k_cache, v_cache, max_nodes, max_len, qkv, logits):
+    i32, f32 = torch.int32, torch.float32
+    H = desc.n_head
+    a = mca_extend_args()
+    _on(dev, i32, "tokens", tokens, 1)
+    n = tokens.numel()
+    _on(dev, i32, "table", table, 2)
+    R = table.shape[0]
+    _flat(dev, i32, "parents", parents, n)
+    _flat(dev, i32, "offsets", offsets, R + 1)
+    _flat(dev, i32, "lengths", lengths, R)
+    if k_cache.dim() != 5 or k_cache.shape[0] != desc.n_block or k_cache.shape[2] != H or k_cache.shape[4] != 32:
+        _refuse(f"k_cache must be [{desc.n_block}, n_blocks, {H}, block_size, 32]")
+    _whole(dev, f32, "k_cache", k_cache, k_cache.shape)
+    _whole(dev, f32, "v_cache", v_cache, k_cache.shape)
+    _whole(dev, f32, "qkv", qkv, (desc.n_block, n, 3, H, 32))
+    _on(dev, f32, "logits", logits, 2)
+    if tuple(logits.shape) != (n, desc.vocab):
+        _refuse(f"logits must be [{n}, {desc.vocab}]")
+    a.n_req, a.n_rows, a.max_nodes = R, n, max_nodes
+    a.n_blocks, a.block_size, a.max_blocks = k_cache.shape[1], k_cache.shape[3], table.shape[1]
+    a.max_len = a.max_blocks * a.block_size if max_len is None else max_len
+    a.table_stride = table.stride(0) if R > 1 else a.max_blocks
+    a.cache_layer = k_cache.stride(0) if desc.n_block > 1 else 0
+    a.logits_row = logits.stride(0) if n > 1 else desc.vocab
+    a.tokens, a.parents, a.offsets = tokens.data_ptr(), parents.data_ptr(), offsets.data_ptr()
+    a.lengths, a.table = lengths.data_ptr(), table.data_ptr()
+    a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
+    a.qkv, a.logits = qkv.data_ptr(), logits.data_ptr()
+    return a
+
+
+def mca_extend(ctx: "mca.TransformerContext", tokens, parents, offsets, lengths, table, k_cache, v_cache, max_nodes: int,
+               max_len: Optional[int] = None, qkv=None, logits=None, workspace=None):
+    """The context's committed net on drafted nodes; returns (logits [n_rows, vocab], qkv [n_block, n_rows, 3, n_head, 32]).
+
+    The work goes on the context's stream: tensors of another stream are the caller's to order.
+    """
+    dev, desc = ctx.device, ctx.desc
+    n = tokens.numel()
+    with torch.cuda.device(dev), torch.cuda.stream(ctx.stream):
+        if qkv is None:
+            qkv = torch.empty((desc.n_block, n, 3, desc.n_head, 32), dtype=torch.float32, device=dev)
+        if logits is None:
+            logits = torch.zeros((n, desc.vocab), dtype=torch.float32, device=dev)
+        a = _extend_args(qkv.device, desc, tokens, parents, offsets, lengths, table, k_cache, v_cache, max_nodes,
+                         max_len, qkv, logits)
+        lib = load_library()
+        nbytes = ctypes.c_size_t(0)
+        _check(lib.mca_extend_plan(ctx.ctx, ctypes.byref(a), ctypes.byref(nbytes)), ctx.ctx)
+        room = _room(qkv.device, nbytes.value, workspace)
+        a.workspace, a.workspace_bytes = room.data_ptr(), room.numel()
+        _check(lib.mca_extend(ctx.ctx, ctypes.byref(a)), ctx.ctx)
+    return logits, qkv

@@ -99,9 +99,55 @@ class mca_timing(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_double * 8), ("launches", ctypes.c_uint64 * 8)]
 
 
-STRUCTS = [mca_net_desc, mca_cand, mca_data, mca_stats, mca_trace, mca_timing, mca_channel]
-
 _P = ctypes.c_void_p
+_I32, _I64 = ctypes.c_int32, ctypes.c_int64
+
+
+# arguments of the language-model operators (include/mca_lm.h; lm.py)
+class mca_cache_append_args(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("dtype", "n_kv_head", "head_dim", "block_size", "n_blocks", "reserved")] + \
+               [("n", _I64), ("n_src", _I64), ("k", _P), ("v", _P)] + \
+               [(n, _I64) for n in ("k_row", "k_head", "v_row", "v_head")] + \
+               [(n, _P) for n in ("k_cache", "v_cache", "slots", "rows")]
+
+
+class mca_tree_attention_args(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("dtype", "n_req", "n_head", "n_kv_head", "head_dim", "block_size", "n_blocks",
+                                    "max_blocks", "max_nodes", "max_len")] + \
+               [("scale", ctypes.c_float), ("reserved", _I32), ("n_rows", _I64), ("table_stride", _I64)] + \
+               [(n, _P) for n in ("q", "k", "v")] + \
+               [(n, _I64) for n in ("q_row", "q_head", "k_row", "k_head", "v_row", "v_head", "out_row", "out_head")] + \
+               [(n, _P) for n in ("k_cache", "v_cache", "table", "lengths", "offsets", "parents", "out", "lse",
+                                  "workspace")] + \
+               [("workspace_bytes", ctypes.c_size_t)]
+
+
+class mca_token_logprobs_args(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("dtype", "n_top", "token_bytes", "reserved")] + \
+               [(n, _I64) for n in ("n_rows", "n_vocab", "logits_row")] + \
+               [(n, _P) for n in ("logits", "tokens", "logprob", "entropy", "lse", "top_logprob", "top_id",
+                                  "workspace")] + \
+               [("workspace_bytes", ctypes.c_size_t)]
+
+
+class mca_token_logprobs_grad_args(ctypes.Structure):
+    _fields_ = [("dtype", _I32), ("token_bytes", _I32)] + \
+               [(n, _I64) for n in ("n_rows", "n_vocab", "logits_row", "grad_row")] + \
+               [(n, _P) for n in ("logits", "tokens", "lse", "entropy", "grad_logprob", "grad_entropy", "grad")]
+
+
+class mca_extend_args(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("n_req", "n_rows", "max_nodes", "max_len", "block_size", "n_blocks", "max_blocks",
+                                    "reserved")] + \
+               [(n, _I64) for n in ("table_stride", "cache_layer", "logits_row")] + \
+               [(n, _P) for n in ("tokens", "parents", "offsets", "lengths", "table", "k_cache", "v_cache", "qkv",
+                                  "logits", "workspace")] + \
+               [("workspace_bytes", ctypes.c_size_t)]
+
+
+STRUCTS = [mca_net_desc, mca_cand, mca_data, mca_stats, mca_trace, mca_timing, mca_channel, mca_cache_append_args,
+           mca_tree_attention_args, mca_token_logprobs_args, mca_token_logprobs_grad_args, mca_extend_args]
+
 _SIGNATURES = {
     "mca_abi_version": (ctypes.c_int, []),
     "mca_struct_size": (ctypes.c_size_t, [ctypes.c_int32]),
@@ -127,6 +173,15 @@ _SIGNATURES = {
     "mca_get_sample_losses": (ctypes.c_int, [_P, _P]),
     "mca_set_timing": (ctypes.c_int, [_P, ctypes.c_int32]),
     "mca_get_timing": (ctypes.c_int, [_P, ctypes.POINTER(mca_timing), ctypes.c_int32]),
+    "mca_block_tables": (ctypes.c_int, [_P, _P, _I32, _I32, _P, _I64, _I32, _P, _I32, _P, _P, _I64, _P, _P]),
+    "mca_cache_append": (ctypes.c_int, [_P, _P]),
+    "mca_tree_attention_plan": (ctypes.c_int, [_P, _P]),
+    "mca_tree_attention": (ctypes.c_int, [_P, _P]),
+    "mca_token_logprobs_plan": (ctypes.c_int, [_P, _P]),
+    "mca_token_logprobs": (ctypes.c_int, [_P, _P]),
+    "mca_token_logprobs_grad": (ctypes.c_int, [_P, _P]),
+    "mca_extend_plan": (ctypes.c_int, [_P, _P, _P]),
+    "mca_extend": (ctypes.c_int, [_P, _P]),
     "mca_destroy": (None, [_P]),
     "mca_last_error": (ctypes.c_char_p, [_P]),
 }
@@ -510,3 +565,8 @@ class TransformerContext(Context):
         self.workspace = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
         self.ctx = mca_init_transformer(desc, params, tokens, targets, k_max, self.workspace,
                                         self.stream.cuda_stream)
+
+    def extend(self, tokens, parents, offsets, lengths, table, k_cache, v_cache, max_nodes, **kw):
+        """The committed net on drafted nodes over a paged cache (lm.mca_extend)."""
+        from . import lm
+        return lm.mca_extend(self, tokens, parents, offsets, lengths, table, k_cache, v_cache, max_nodes, **kw)

@@ -55,9 +55,9 @@ const char* lm_check_attention(const mca_tree_attention_args& a, int* code) {
   if ((int64_t)a.max_blocks * a.block_size > kMaxInt || a.max_len > kMaxInt) return "cached tokens must stay below 2^31 - 1";
   if ((int64_t)a.n_blocks * a.n_kv_head > kMaxInt || (int64_t)a.n_blocks * a.n_kv_head * a.block_size > kMaxInt)
     return "n_blocks * n_kv_head * block_size must stay below 2^31 - 1";
-  // workgroups: at least 16 rows each
+  // workgroups: at least 16 rows each, and a few thousand more when split
   const int64_t tiles = ((int64_t)a.max_nodes * (a.n_head / a.n_kv_head) + 15) / 16;
-  if (tiles > kMaxGrid || tiles * a.n_kv_head > kMaxGrid || tiles * a.n_kv_head * a.n_req > kMaxGrid ||
+  if (tiles > kMaxGrid / 16 || tiles * a.n_kv_head > kMaxGrid / 2 || tiles * a.n_kv_head * a.n_req > kMaxGrid / 2 ||
       (int64_t)a.n_head * a.max_nodes > kMaxGrid)
     return "too many requests times heads for one call";
   *code = MCA_OK;
@@ -127,6 +127,7 @@ int mca_tree_attention(const mca_tree_attention_args* args, void* hip_stream) {
   if (!strides_ok({a.q_row, a.q_head, a.k_row, a.k_head, a.v_row, a.v_head, a.out_row, a.out_head, a.table_stride}, kMaxStride) ||
       a.table_stride < a.max_blocks)
     return invalid("strides must not be negative, table_stride at least max_blocks");
+  if (a.k_row * el > 0x7fffffff || a.v_row * el > 0x7fffffff) return unsupported("rows of k and v must be less than 2^31 bytes apart");
   if (a.n_req == 0 || a.n_rows == 0) return MCA_OK;
   if (!a.q || !a.k || !a.v || !a.out || !a.k_cache || !a.v_cache || !a.lengths || !a.offsets || !a.parents ||
       (!a.table && a.max_blocks > 0))

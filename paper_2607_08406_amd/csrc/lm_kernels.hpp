@@ -27,9 +27,10 @@ hipError_t lm_launch_tables(const TablesArgs& a, hipStream_t s);
 hipError_t lm_launch_append(const mca_cache_append_args& a, hipStream_t s);
 
 // How the attention call is split: chunks of `chunk` cached tokens, at most
-// `splits` of them for a request; partial results take `bytes` of workspace.
+// `splits` of them for a request, or evenly over `sharers` workgroups where that
+// is not 0; partial results take `bytes` of workspace.
 struct AttnPlan {
-  int32_t chunk, splits;
+  int32_t chunk, splits, sharers;
   size_t bytes;
 };
 AttnPlan lm_attention_plan(const mca_tree_attention_args& a);

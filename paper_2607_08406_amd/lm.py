@@ -9,10 +9,10 @@ given.  Nothing is synchronised.
 from __future__ import annotations
 
 import ctypes
-import math
 from typing import NamedTuple, Optional
 
 import torch
+from torch._C import _cuda_getCurrentRawStream as _raw_stream
 
 from . import mca
 from .mca import (MCA_EDEVICE, MCA_EINVAL, MCAError, _check, load_library, mca_cache_append_args, mca_extend_args,
@@ -36,27 +36,40 @@ def _type(t: torch.Tensor) -> int:
     return code
 
 
-def _on(device, dtype, what, t, dim):
-    """t is a tensor of that device, type and number of dimensions, the last one contiguous."""
-    if t.device != device:
-        _refuse(f"{what} is on {t.device}, not {device}")
-    if t.dtype != dtype:
-        _refuse(f"{what} holds {t.dtype}, not {dtype}")
-    if t.dim() != dim:
-        _refuse(f"{what} has {t.dim()} dimensions, not {dim}")
-    if dim and t.stride(-1) != 1 and t.size(-1) > 1:
-        _refuse(f"{what} is not contiguous in its last dimension")
+def _check_all(device, dtype, dim, **tensors):
+    """Each tensor is on that device, of that type and number of dimensions, the last one contiguous."""
+    for what, t in tensors.items():
+        if t.device != device:
+            _refuse(f"{what} is on {t.device}, not {device}")
+        if t.dtype != dtype:
+            _refuse(f"{what} holds {t.dtype}, not {dtype}")
+        if t.dim() != dim:
+            _refuse(f"{what} has {t.dim()} dimensions, not {dim}")
+        if t.stride(-1) != 1 and t.size(-1) > 1:
+            _refuse(f"{what} is not contiguous in its last dimension")
 
 
 def _flat(device, dtype, what, t, size):
-    _on(device, dtype, what, t, 1)
+    if t.dtype is not dtype or t.dim() != 1 or t.device != device or not t.is_contiguous():
+        _check_all(device, dtype, 1, **{what: t})
     if t.numel() != size:
         _refuse(f"{what} has {t.numel()} entries, not {size}")
 
 
+def _rows(device, dtype, what, t, shape):
+    """The strides of a tensor of that shape, whose last dimension is contiguous."""
+    if t.dtype is not dtype or t.device != device or t.shape != shape:
+        _check_all(device, dtype, len(shape), **{what: t})
+        _refuse(f"{what} has shape {tuple(t.shape)}, not {tuple(shape)}")
+    s = t.stride()
+    if s[-1] != 1 and shape[-1] > 1:
+        _refuse(f"{what} is not contiguous in its last dimension")
+    return s
+
+
 def _whole(device, dtype, what, t, shape):
-    _on(device, dtype, what, t, len(shape))
-    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+    if t.dtype is not dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+        _check_all(device, dtype, len(shape), **{what: t})
         _refuse(f"{what} is not a contiguous tensor of shape {tuple(shape)}")
 
 
@@ -66,22 +79,22 @@ def _gpu(t: torch.Tensor) -> torch.device:
     return t.device
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
-
-
 def _run(device, call, *args):
-    if torch.cuda.current_device() == device.index:
-        _check(call(*args, _stream(device)))
+    # the raw handle: a Stream object would cost as much host time as the launch
+    index = device.index
+    if torch.cuda.current_device() == index:
+        rc = call(*args, _raw_stream(index))
     else:
         with torch.cuda.device(device):
-            _check(call(*args, _stream(device)))
+            rc = call(*args, _raw_stream(index))
+    if rc:
+        _check(rc)
 
 
 def _room(device, nbytes, workspace):
     if workspace is None:
         return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    _on(device, torch.uint8, "workspace", workspace, 1)
+    _flat(device, torch.uint8, "workspace", workspace, workspace.numel())
     return workspace
 
 
@@ -93,16 +106,16 @@ def mca_block_tables(old_len, new_len, table, free_list, block_size: int, offset
     """Update table [n_req, max_blocks] and free_list [n_blocks] for requests that go from old_len to
     new_len [n_req] tokens; offsets [n_req + 1], slots [max_tokens] (int64) and status [4] are written."""
     dev, i32 = _gpu(table), torch.int32
-    _on(dev, i32, "table", table, 2)
-    n = table.shape[0]
+    _check_all(dev, i32, 2, table=table)
+    n, width = table.shape
     _flat(dev, i32, "old_len", old_len, n)
     _flat(dev, i32, "new_len", new_len, n)
-    _on(dev, i32, "free_list", free_list, 1)
+    _flat(dev, i32, "free_list", free_list, free_list.numel())
     _flat(dev, i32, "offsets", offsets, n + 1)
-    _on(dev, torch.int64, "slots", slots, 1)
+    _flat(dev, torch.int64, "slots", slots, slots.numel())
     _flat(dev, i32, "status", status, 4)
     _run(dev, load_library().mca_block_tables, old_len.data_ptr(), new_len.data_ptr(), n, block_size, table.data_ptr(),
-         table.stride(0) if n > 1 else table.shape[1], table.shape[1], free_list.data_ptr(), free_list.numel(),
+         table.stride(0) if n > 1 else width, width, free_list.data_ptr(), free_list.numel(),
          offsets.data_ptr(), slots.data_ptr(), slots.numel(), status.data_ptr())
 
 
@@ -114,23 +127,22 @@ def mca_cache_append(k, v, k_cache, v_cache, slots, rows=None):
     a.dtype = _type(k_cache)
     if k_cache.dim() != 4:
         _refuse("k_cache has 4 dimensions")
-    _whole(dev, dt, "k_cache", k_cache, k_cache.shape)
-    _whole(dev, dt, "v_cache", v_cache, k_cache.shape)
-    _on(dev, dt, "k", k, 3)
-    _on(dev, dt, "v", v, 3)
-    a.n_blocks, a.n_kv_head, a.block_size, a.head_dim = k_cache.shape
-    if k.shape != v.shape or tuple(k.shape[1:]) != (a.n_kv_head, a.head_dim):
-        _refuse("k and v must be [n_src, n_kv_head, head_dim] like the caches' heads")
-    _on(dev, torch.int64, "slots", slots, 1)
-    a.n, a.n_src = slots.numel(), k.shape[0]
+    shape = k_cache.shape
+    _whole(dev, dt, "k_cache", k_cache, shape)
+    _whole(dev, dt, "v_cache", v_cache, shape)
+    a.n_blocks, a.n_kv_head, a.block_size, a.head_dim = shape
+    n, n_src = slots.numel(), k.shape[0] if k.dim() else 0
+    src = (n_src, shape[1], shape[3])
+    a.k_row, a.k_head, _ = _rows(dev, dt, "k", k, src)
+    a.v_row, a.v_head, _ = _rows(dev, dt, "v", v, src)
+    _flat(dev, torch.int64, "slots", slots, n)
+    a.n, a.n_src = n, n_src
     if rows is not None:
-        _flat(dev, torch.int32, "rows", rows, a.n)
+        _flat(dev, torch.int32, "rows", rows, n)
         a.rows = rows.data_ptr()
-    elif a.n != a.n_src:
+    elif n != n_src:
         _refuse("without rows, slots has an entry for each row of k")
     a.k, a.v, a.k_cache, a.v_cache = k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr()
-    a.k_row, a.k_head, _ = k.stride()
-    a.v_row, a.v_head, _ = v.stride()
     a.slots = slots.data_ptr()
     _run(dev, load_library().mca_cache_append, ctypes.byref(a))
 
@@ -143,37 +155,34 @@ def _attention_args(q, k, v, k_cache, v_cache, table, lengths, offsets, parents,
     dev, dt, i32 = _gpu(q), q.dtype, torch.int32
     a = mca_tree_attention_args()
     a.dtype = _type(q)
-    _on(dev, dt, "q", q, 3)
-    _on(dev, dt, "k", k, 3)
-    _on(dev, dt, "v", v, 3)
-    if k_cache.dim() != 4:
-        _refuse("k_cache has 4 dimensions")
-    _whole(dev, dt, "k_cache", k_cache, k_cache.shape)
-    _whole(dev, dt, "v_cache", v_cache, k_cache.shape)
-    a.n_rows, a.n_head, a.head_dim = q.shape
-    a.n_blocks, a.n_kv_head, a.block_size, dim = k_cache.shape
-    if k.shape != v.shape or tuple(k.shape) != (a.n_rows, a.n_kv_head, a.head_dim) or dim != a.head_dim:
-        _refuse("q, k, v and the caches must agree in rows, heads and head_dim")
-    _on(dev, i32, "table", table, 2)
-    a.n_req, a.max_blocks = table.shape
-    _flat(dev, i32, "lengths", lengths, a.n_req)
-    _flat(dev, i32, "offsets", offsets, a.n_req + 1)
-    _flat(dev, i32, "parents", parents, a.n_rows)
-    _on(dev, dt, "out", out, 3)
-    if out.shape != q.shape:
-        _refuse("out must have q's shape")
+    if q.dim() != 3 or k_cache.dim() != 4 or table.dim() != 2:
+        _refuse("q has 3 dimensions, k_cache 4, table 2")
+    shape, cache = q.shape, k_cache.shape
+    n, n_head, dim = shape
+    n_blocks, n_kv_head, block_size, _ = cache
+    if cache[3] != dim:
+        _refuse("q and the caches must agree in head_dim")
+    a.q_row, a.q_head, _ = _rows(dev, dt, "q", q, shape)
+    a.k_row, a.k_head, _ = _rows(dev, dt, "k", k, (n, n_kv_head, dim))
+    a.v_row, a.v_head, _ = _rows(dev, dt, "v", v, (n, n_kv_head, dim))
+    a.out_row, a.out_head, _ = _rows(dev, dt, "out", out, shape)
+    _whole(dev, dt, "k_cache", k_cache, cache)
+    _whole(dev, dt, "v_cache", v_cache, cache)
+    n_req, max_blocks = table.shape
+    stride = _rows(dev, i32, "table", table, table.shape)[0]
+    _flat(dev, i32, "lengths", lengths, n_req)
+    _flat(dev, i32, "offsets", offsets, n_req + 1)
+    _flat(dev, i32, "parents", parents, n)
     if lse is not None:
-        _whole(dev, torch.float32, "lse", lse, q.shape[:2])
+        _whole(dev, torch.float32, "lse", lse, shape[:2])
         a.lse = lse.data_ptr()
-    a.max_nodes = max_nodes
-    a.max_len = a.max_blocks * a.block_size if max_len is None else max_len
-    a.scale = 1.0 / math.sqrt(a.head_dim) if scale is None else scale
-    a.table_stride = table.stride(0) if a.n_req > 1 else a.max_blocks
+    a.n_rows, a.n_head, a.head_dim = n, n_head, dim
+    a.n_blocks, a.n_kv_head, a.block_size = n_blocks, n_kv_head, block_size
+    a.n_req, a.max_blocks, a.max_nodes = n_req, max_blocks, max_nodes
+    a.max_len = max_blocks * block_size if max_len is None else max_len
+    a.scale = dim ** -0.5 if scale is None else scale
+    a.table_stride = stride if n_req > 1 else max_blocks
     a.q, a.k, a.v, a.out = q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr()
-    a.q_row, a.q_head, _ = q.stride()
-    a.k_row, a.k_head, _ = k.stride()
-    a.v_row, a.v_head, _ = v.stride()
-    a.out_row, a.out_head, _ = out.stride()
     a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()
     a.table, a.lengths = table.data_ptr(), lengths.data_ptr()
     a.offsets, a.parents = offsets.data_ptr(), parents.data_ptr()
@@ -235,12 +244,16 @@ class TokenLogprobs(NamedTuple):
 
 
 def _logits(logits, tokens):
+    """The logits' device and row stride."""
     dev = _gpu(logits)
-    _on(dev, logits.dtype, "logits", logits, 2)
-    if tokens.dtype not in (torch.int32, torch.int64):
+    if logits.dim() != 2:
+        _refuse("logits has 2 dimensions")
+    row = _rows(dev, logits.dtype, "logits", logits, logits.shape)[0]
+    if tokens.dtype is not torch.int32 and tokens.dtype is not torch.int64:
         _refuse("tokens must be int32 or int64")
-    _flat(dev, tokens.dtype, "tokens", tokens, logits.shape[0])
-    return dev, logits.stride(0) if logits.shape[0] > 1 else logits.shape[1]
+    n, n_vocab = logits.shape
+    _flat(dev, tokens.dtype, "tokens", tokens, n)
+    return dev, row if n > 1 else n_vocab
 
 
 def mca_token_logprobs_plan(logits, n_top: int = 0) -> int:
@@ -260,17 +273,17 @@ def mca_token_logprobs(logits, tokens, n_top: int = 0, workspace=None) -> TokenL
     a.n_rows, a.logits_row = n, row
     lib = load_library()
     nbytes = _plan(a, lib.mca_token_logprobs_plan)
-    f = torch.empty((3, n), dtype=torch.float32, device=dev)
+    logprob, entropy, lse = torch.empty((3, n), dtype=torch.float32, device=dev).unbind()
     top = torch.empty((n, n_top), dtype=torch.float32, device=dev)
     ids = torch.empty((n, n_top), dtype=torch.int32, device=dev)
     a.logits, a.tokens = logits.data_ptr(), tokens.data_ptr()
-    a.logprob, a.entropy, a.lse = f[0].data_ptr(), f[1].data_ptr(), f[2].data_ptr()
+    a.logprob, a.entropy, a.lse = logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr()
     a.top_logprob, a.top_id = top.data_ptr(), ids.data_ptr()
     if nbytes:
         room = _room(dev, nbytes, workspace)
         a.workspace, a.workspace_bytes = room.data_ptr(), room.numel()
     _run(dev, lib.mca_token_logprobs, ctypes.byref(a))
-    return TokenLogprobs(f[0], f[1], f[2], top, ids)
+    return TokenLogprobs(logprob, entropy, lse, top, ids)
 
 
 def mca_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, grad_entropy=None, out=None):
@@ -279,13 +292,11 @@ def mca_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, gra
     n, f32 = logits.shape[0], torch.float32
     if out is None:
         out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-    _on(dev, logits.dtype, "out", out, 2)
-    if out.shape != logits.shape:
-        _refuse("out must have the logits' shape")
+    grad_row = _rows(dev, logits.dtype, "out", out, logits.shape)[0]
     a = mca_token_logprobs_grad_args()
     a.dtype, a.token_bytes = _type(logits), tokens.element_size()
     a.n_rows, a.n_vocab = logits.shape
-    a.logits_row, a.grad_row = row, out.stride(0) if n > 1 else out.shape[1]
+    a.logits_row, a.grad_row = row, grad_row if n > 1 else out.shape[1]
     a.logits, a.tokens, a.grad = logits.data_ptr(), tokens.data_ptr(), out.data_ptr()
     _flat(dev, f32, "lse", lse, n)
     a.lse = lse.data_ptr()
@@ -308,9 +319,9 @@ def _extend_args(dev, desc, tokens, parents, offsets, lengths, table, k_cache, v
     i32, f32 = torch.int32, torch.float32
     H = desc.n_head
     a = mca_extend_args()
-    _on(dev, i32, "tokens", tokens, 1)
     n = tokens.numel()
-    _on(dev, i32, "table", table, 2)
+    _flat(dev, i32, "tokens", tokens, n)
+    _check_all(dev, i32, 2, table=table)
     R = table.shape[0]
     _flat(dev, i32, "parents", parents, n)
     _flat(dev, i32, "offsets", offsets, R + 1)
@@ -320,15 +331,13 @@ def _extend_args(dev, desc, tokens, parents, offsets, lengths, table, k_cache, v
     _whole(dev, f32, "k_cache", k_cache, k_cache.shape)
     _whole(dev, f32, "v_cache", v_cache, k_cache.shape)
     _whole(dev, f32, "qkv", qkv, (desc.n_block, n, 3, H, 32))
-    _on(dev, f32, "logits", logits, 2)
-    if tuple(logits.shape) != (n, desc.vocab):
-        _refuse(f"logits must be [{n}, {desc.vocab}]")
+    logits_row = _rows(dev, f32, "logits", logits, (n, desc.vocab))[0]
     a.n_req, a.n_rows, a.max_nodes = R, n, max_nodes
     a.n_blocks, a.block_size, a.max_blocks = k_cache.shape[1], k_cache.shape[3], table.shape[1]
     a.max_len = a.max_blocks * a.block_size if max_len is None else max_len
     a.table_stride = table.stride(0) if R > 1 else a.max_blocks
     a.cache_layer = k_cache.stride(0) if desc.n_block > 1 else 0
-    a.logits_row = logits.stride(0) if n > 1 else desc.vocab
+    a.logits_row = logits_row if n > 1 else desc.vocab
     a.tokens, a.parents, a.offsets = tokens.data_ptr(), parents.data_ptr(), offsets.data_ptr()
     a.lengths, a.table = lengths.data_ptr(), table.data_ptr()
     a.k_cache, a.v_cache = k_cache.data_ptr(), v_cache.data_ptr()

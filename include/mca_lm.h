@@ -142,7 +142,8 @@ int mca_tree_attention(const mca_tree_attention_args* args, void* hip_stream);
  * logits of -inf have probability 0 and no part in the entropy.  A token
  * outside [0, n_vocab) is none: logprob 0.  A row of nothing but -inf gives
  * lse = -inf, entropy 0, and -inf for logprob and alternatives; a NaN or +inf
- * makes the row's floating results NaN and its alternatives' order unspecified.  tokens are int32, or int64 with token_bytes 8. */
+ * makes the row's floating results NaN and its alternatives unspecified (symbols
+ * of the vocabulary).  tokens are int32, or int64 with token_bytes 8. */
 typedef struct mca_token_logprobs_args {
   int32_t dtype, n_top, token_bytes, reserved;
   int64_t n_rows, n_vocab, logits_row;

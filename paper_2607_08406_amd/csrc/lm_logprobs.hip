@@ -24,9 +24,10 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kLpThreads = 256;
 constexpr int kLpWaves = kLpThreads / 64;
 constexpr int kLpUnroll = 4;     // 16-byte loads that a lane has in flight
-constexpr int kLpBuf = 320;      // chunks that a wave holds as candidates
+constexpr int kLpBuf = 128;      // chunks that a wave holds as candidates: thinned when over 64
 constexpr int kLpSmall = 1024;   // largest vocabulary of the wave-per-row kernel
 constexpr int kLpSplits = 64;    // most parts of a row
+constexpr int64_t kLpPart = 8192;   // symbols of a part at least
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kFar = -1e30f;   // below every exponent; times 0 it is 0
 constexpr float kHuge = 1e38f;   // logits of this size times log2 e stay finite
@@ -73,6 +74,13 @@ __device__ __forceinline__ uint32_t sort_key(float x) {
   const uint32_t b = __float_as_uint(x + 0.0f);
   return max(b ^ ((b >> 31) ? 0xffffffffu : 0x80000000u), 1u);
 }
+// The part of the order that a type's values differ in: its last bits are all
+// zeros (or, of negative values, ones), and a bisection does without them.
+template <int TYPE>
+__device__ __forceinline__ uint32_t short_key(float x) {
+  constexpr int kSame = TYPE == MCA_TYPE_F32 ? 0 : (TYPE == MCA_TYPE_BF16 ? 16 : 13);
+  return max(sort_key(x) >> kSame, 1u);
+}
 __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float(k ^ ((k >> 31) ? 0x80000000u : 0xffffffffu));
 }
@@ -85,6 +93,19 @@ __device__ __forceinline__ void wave_sync() {
 }
 __device__ __forceinline__ int lanes_below(uint64_t mask) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+// How many of n keys in LDS go before `key`; behind the n, zeros up to a multiple
+// of 8, so that eight are under way at a time.
+__device__ __forceinline__ int keys_above(const uint64_t* keys, int n, uint64_t key) {
+  int before = 0;
+  for (int i = 0; i < n; i += 8) {
+    uint64_t x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] = keys[i + u];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) before += x[u] > key;
+  }
+  return before;
 }
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
@@ -149,39 +170,88 @@ __device__ __forceinline__ void finish_row(const mca_token_logprobs_args& p, int
   p.logprob[t] = tok < 0 || tok >= p.n_vocab ? 0.f : logprob_of(a, to_f32<TYPE>(row[tok]));
 }
 
-// Of cnt <= kLpBuf (key, id) pairs in LDS, ids rising, keeps the k with the
-// largest keys, of equal ones the first; the order stays.  One wave.  The k-th
-// largest key is found bit by bit from the top.
-__device__ __forceinline__ int keep_largest(uint32_t* key, uint32_t* id, int cnt, int k, uint32_t* least) {
-  constexpr int kPer = kLpBuf / 64;
+// an alternative that a row (with NaN) lacks
+__device__ __forceinline__ void no_choice(const mca_token_logprobs_args& p, int64_t t, int n) {
+  p.top_logprob[t * p.n_top + n] = __builtin_nanf("");
+  p.top_id[t * p.n_top + n] = 0;
+}
+
+// A key that at least k and, if they are not equal, at most `most` of the wave's
+// 64 keys reach, by bisection.
+__device__ __forceinline__ uint32_t reached_by(uint32_t key, int k, int most) {
+  uint32_t lo = key, hi = key;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor(lo, d, 64));
+    hi = max(hi, (uint32_t)__shfl_xor(hi, d, 64));
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  int reach = 64;
+  while (reach > most && lo < hi) {
+    const uint32_t mid = lo + (hi - lo + 1) / 2;
+    const int c = __popcll(__ballot(key >= mid));
+    if (c >= k) {
+      lo = mid;
+      reach = c;
+    } else {
+      hi = mid - 1;
+    }
+  }
+  return lo;
+}
+
+// Of cnt <= 64 N (key, id) pairs in LDS, ids rising, keeps at most `most` among
+// which are the k with the largest keys, of equal ones the first; the order stays.
+// One wave.  *least becomes a key that at least k of them reach.  It is found by
+// bisection, which ends as soon as few enough reach it; only where so many keys are
+// equal that none does are those thinned by their order.
+template <int N>
+__device__ __forceinline__ int keep_largest(uint32_t* key, uint32_t* id, int cnt, int k, int most, uint32_t* least) {
   const int lane = threadIdx.x & 63;
   wave_sync();
-  uint32_t kk[kPer], ii[kPer];
+  if (cnt <= most) return cnt;
+  uint32_t kk[N], ii[N], lo = 0xffffffffu, hi = 0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
+  for (int i = 0; i < N; ++i) {
     const int p = 64 * i + lane;
     kk[i] = p < cnt ? key[p] : 0;
     ii[i] = p < cnt ? id[p] : 0;
+    lo = min(lo, p < cnt ? kk[i] : 0xffffffffu);
+    hi = max(hi, kk[i]);
   }
-  if (cnt <= k) return cnt;
-  uint32_t T = 0;
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t c = T | (1u << bit);
-    int over = 0;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) over += __popcll(__ballot(kk[i] >= c));
-    if (over >= k) T = c;
+  for (int d = 1; d < 64; d <<= 1) {
+    lo = min(lo, (uint32_t)__shfl_xor(lo, d, 64));
+    hi = max(hi, (uint32_t)__shfl_xor(hi, d, 64));
   }
-  int gt = 0;
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  int reach = cnt;  // keys of at least lo; fewer than k are above hi
+  while (reach > most && lo < hi) {
+    const uint32_t mid = lo + (hi - lo + 1) / 2;
+    int c = 0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) gt += __popcll(__ballot(kk[i] > T));
+    for (int i = 0; i < N; ++i) c += __popcll(__ballot(kk[i] >= mid));
+    if (c >= k) {
+      lo = mid;
+      reach = c;
+    } else {
+      hi = mid - 1;
+    }
+  }
+  int equal = reach;  // how many keys equal to lo are kept
+  if (reach > most) {
+    equal = k;
+#pragma unroll
+    for (int i = 0; i < N; ++i) equal -= __popcll(__ballot(kk[i] > lo));
+  }
   int eq = 0, out = 0;
-  wave_sync();
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const bool same = kk[i] == T && 64 * i + lane < cnt;
+  for (int i = 0; i < N; ++i) {
+    const bool same = kk[i] == lo && 64 * i + lane < cnt;
     const uint64_t es = __ballot(same);
-    const bool keep = kk[i] > T || (same && eq + lanes_below(es) < k - gt);
+    const bool keep = kk[i] > lo || (same && eq + lanes_below(es) < equal);
     const uint64_t ks = __ballot(keep);
     if (keep) {
       const int at = out + lanes_below(ks);
@@ -192,8 +262,8 @@ __device__ __forceinline__ int keep_largest(uint32_t* key, uint32_t* id, int cnt
     out += __popcll(ks);
   }
   wave_sync();
-  *least = T;
-  return k;
+  *least = lo;
+  return out;
 }
 
 }  // namespace
@@ -206,17 +276,16 @@ __device__ __forceinline__ int keep_largest(uint32_t* key, uint32_t* id, int cnt
 // the k chunks of largest maximum (equal ones: the first), because each of
 // those maxima is a value.  So the pass compares one maximum per chunk with the
 // k-th largest so far, and only larger ones go to the wave's buffer, which is
-// thinned to k when it is full; the values of the k chunks are read again at the
-// end.
+// thinned to about k when it is full; the chunks left are read again at the end.
 template <int TYPE, bool TOP>
 __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs(mca_token_logprobs_args p, int splits, Sums* part,
                                                             uint64_t* part_keys) {
   constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
   typedef typename Elem<TYPE>::Raw Raw;
   __shared__ uint32_t s_key[TOP ? kLpWaves : 1][TOP ? kLpBuf : 1], s_id[TOP ? kLpWaves : 1][TOP ? kLpBuf : 1];
-  __shared__ uint64_t s_rank[TOP ? 256 : 1];
-  __shared__ uint32_t s_chunk[MCA_MAX_TOP];
-  __shared__ int s_cnt[kLpWaves];
+  __shared__ __attribute__((aligned(16))) uint64_t s_rank[TOP ? 64 * kLpWaves * VE + 8 : 1];
+  __shared__ uint32_t s_least[kLpWaves];
+  __shared__ int s_found;
   __shared__ Sums s_sums[kLpWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t = blockIdx.x;
@@ -227,38 +296,44 @@ __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs(mca_token_logprobs_a
   const u32x4* vec = (const u32x4*)(row + head);
   const int per = (nvec + splits - 1) / splits, v0 = min(split * per, nvec), v1 = min(nvec, v0 + per);
   Sums a = {kLowest, 0.f, 0.f};
-  int cnt = 0;
-  float thr = -__builtin_huge_valf();
+  int cnt = 0;       // chunks held
+  uint32_t thr = 0;  // only maxima of larger keys are taken: the wave has k that reach it
   // one chunk a lane; `here` lanes have one
   auto take = [&](const float (&f)[VE], bool here, int id) {
     float cm = f[0];
 #pragma unroll
     for (int i = 1; i < VE; ++i) cm = fmaxf(cm, f[i]);
     if (__ballot(here && cm > a.m) != 0) a = moved(a, wave_max(here ? fmaxf(cm, a.m) : a.m));
-    auto add = [&](bool plain) {
+    // 0 times the exponent of a logit of -inf has to be 0, which a bound on the
+    // exponent gives; only chunks with such logits pay for it
+    float low = f[0];
+#pragma unroll
+    for (int i = 1; i < VE; ++i) low = fminf(low, f[i]);
+    auto add = [&](bool plain, bool bounded) {
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
         const float y = exponent(f[i], a.m, plain), e = __builtin_amdgcn_exp2f(y);
         a.s += e;
-        a.w = fmaf(e, fmaxf(y, kFar), a.w);
+        a.w = fmaf(e, bounded ? fmaxf(y, kFar) : y, a.w);
       }
     };
-    if (here) {
-      if (ordinary(a.m)) add(true); else add(false);
+    if (ordinary(a.m) && __ballot(here && low < kFar) == 0) {
+      if (here) add(true, false);
+    } else if (here) {
+      if (ordinary(a.m)) add(true, true); else add(false, true);
     }
     if constexpr (TOP) {
-      const uint64_t mask = __ballot(here && (cm > thr || cnt < k));
+      const uint32_t key = short_key<TYPE>(cm);
+      const uint64_t mask = __ballot(here && key > thr);
       if (mask != 0) {
         if ((mask >> lane) & 1) {
           const int at = cnt + lanes_below(mask);
-          s_key[wave][at] = sort_key(cm);
+          s_key[wave][at] = key;
           s_id[wave][at] = (uint32_t)id;
         }
         cnt += __popcll(mask);
         if (cnt > kLpBuf - 64) {
-          uint32_t least = 0;
-          cnt = keep_largest(s_key[wave], s_id[wave], cnt, k, &least);
-          thr = key_value(least);
+          cnt = keep_largest<kLpBuf / 64>(s_key[wave], s_id[wave], cnt, k, max(k + 8, 16), &thr);
         }
       }
     }
@@ -275,6 +350,19 @@ __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs(mca_token_logprobs_a
     u32x4 x[kLpUnroll];
 #pragma unroll
     for (int u = 0; u < kLpUnroll; ++u) x[u] = gload(vec + min(b + 64 * u + lane, v1 - 1));
+    if (TOP && thr == 0 && b + 64 * kLpUnroll <= v1) {
+      // the first whole round: at least k lanes reach the k-th largest of the lanes'
+      // maxima, which spares the buffer most of the round
+      float top = -__builtin_huge_valf();
+#pragma unroll
+      for (int u = 0; u < kLpUnroll; ++u) {
+        float f[VE];
+        unpack<TYPE>(x[u], f);
+#pragma unroll
+        for (int i = 0; i < VE; ++i) top = fmaxf(top, f[i]);
+      }
+      thr = reached_by(short_key<TYPE>(top), k, max(k + 8, 16)) - 1;  // that key itself is taken
+    }
 #pragma unroll
     for (int u = 0; u < kLpUnroll; ++u) {
       const int v = b + 64 * u + lane;
@@ -286,10 +374,14 @@ __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs(mca_token_logprobs_a
   if (tail > 0 && split == splits - 1 && wave == kLpWaves - 1) take_part(V - tail, tail, nvec + 1);
   a = wave_join(a);
   if (lane == 0) s_sums[wave] = a;
+  uint32_t mine = 0;
   if constexpr (TOP) {
-    uint32_t least;
-    cnt = keep_largest(s_key[wave], s_id[wave], cnt, k, &least);
-    if (lane == 0) s_cnt[wave] = cnt;
+    // the wave's chunks, at most 64, one a lane, and a key that k of them reach
+    wave_sync();
+    mine = lane < cnt ? s_key[wave][lane] : 0;
+    const uint32_t least = cnt >= k ? reached_by(mine, k, k + 8) : 0;
+    if (lane == 0) s_least[wave] = least;
+    if (tid == 0) s_found = 0;
   }
   __syncthreads();
   a = s_sums[0];
@@ -302,47 +394,46 @@ __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs(mca_token_logprobs_a
       part[t * splits + split] = a;
   }
   if constexpr (TOP) {
-    // the k first of the waves' chunks, each thread counting how many go before its own
-    int all = 0, mine = -1, at = 0;
+    // The largest of those keys is one that k values reach, so only values that do
+    // are ranked: k and a few, but for equal ones.
+    uint32_t least = s_least[0];
 #pragma unroll
-    for (int w = 0; w < kLpWaves; ++w) {
-      if (tid >= all && tid < all + s_cnt[w]) {
-        mine = w;
-        at = tid - all;
-      }
-      all += s_cnt[w];
-    }
-    uint64_t key = mine >= 0 ? rank_key(s_key[mine][at], s_id[mine][at]) : 0;
-    s_rank[tid] = key;
-    __syncthreads();
-    if (mine >= 0) {
-      int before = 0;
-      for (int i = 0; i < all; ++i) before += s_rank[i] > key;
-      if (before < k) s_chunk[before] = s_id[mine][at];
-    }
-    __syncthreads();
-    // their values likewise
-    const int chunks = min(k, all), c = tid / VE, e = tid - c * VE;
-    key = 0;
-    if (c < chunks) {
-      const int id = (int)s_chunk[c];
+    for (int w = 1; w < kLpWaves; ++w) least = max(least, s_least[w]);
+    if (mine != 0 && mine >= least) {
+      const int id = (int)s_id[wave][lane];
       const int v = id == 0 ? 0 : head + (id - 1) * VE;
-      const int n = id == 0 ? head : (id == nvec + 1 ? tail : VE);
-      if (e < n) key = rank_key(sort_key(to_f32<TYPE>(row[v + e])), (uint32_t)(v + e));
+      float f[VE];
+      if (id == 0 || id > nvec) {
+        const int n = id == 0 ? head : tail;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) f[i] = to_f32<TYPE>(row[v + min(i, n - 1)]);
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+          if (i < n && short_key<TYPE>(f[i]) >= least) s_rank[atomicAdd(&s_found, 1)] = rank_key(sort_key(f[i]), (uint32_t)(v + i));
+      } else {
+        unpack<TYPE>(gload(vec + id - 1), f);
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+          if (short_key<TYPE>(f[i]) >= least) s_rank[atomicAdd(&s_found, 1)] = rank_key(sort_key(f[i]), (uint32_t)(v + i));
+      }
     }
-    s_rank[tid] = key;
-    const int found = __syncthreads_count(key != 0);
-    if (splits > 1 && tid >= found && tid < k) part_keys[(t * splits + split) * k + tid] = 0;
-    if (key != 0) {
-      int before = 0;
-      for (int i = 0; i < chunks * VE; ++i) before += s_rank[i] > key;
-      if (before < k) {
-        if (splits == 1) {
-          p.top_logprob[t * k + before] = logprob_of(a, key_value((uint32_t)(key >> 32)));
-          p.top_id[t * k + before] = (int32_t)~(uint32_t)key;
-        } else {
-          part_keys[(t * splits + split) * k + before] = key;
-        }
+    __syncthreads();
+    const int found = s_found;
+    if (tid < 8) s_rank[found + tid] = 0;
+    // behind the last: nothing of a part, and in a row with NaN something in bounds
+    if (tid >= found && tid < k) {
+      if (splits > 1) part_keys[(t * splits + split) * k + tid] = 0; else no_choice(p, t, tid);
+    }
+    __syncthreads();
+    for (int i = tid; i < found; i += kLpThreads) {
+      const uint64_t key = s_rank[i];
+      const int before = keys_above(s_rank, found, key);
+      if (before >= k) continue;
+      if (splits == 1) {
+        p.top_logprob[t * k + before] = logprob_of(a, key_value((uint32_t)(key >> 32)));
+        p.top_id[t * k + before] = (int32_t)~(uint32_t)key;
+      } else {
+        part_keys[(t * splits + split) * k + before] = key;
       }
     }
   }
@@ -354,7 +445,7 @@ __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs(mca_token_logprobs_a
 template <int TYPE>
 __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs_join(mca_token_logprobs_args p, int splits, const Sums* part,
                                                                  const uint64_t* part_keys) {
-  __shared__ uint64_t s_rank[kLpSplits * MCA_MAX_TOP];
+  __shared__ __attribute__((aligned(16))) uint64_t s_rank[kLpSplits * MCA_MAX_TOP + 8];
   __shared__ int s_cnt;
   const int tid = threadIdx.x, lane = tid & 63, k = p.n_top;
   const int64_t t = blockIdx.x;
@@ -379,10 +470,12 @@ __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs_join(mca_token_logpr
   }
   __syncthreads();
   const int n = s_cnt;
+  if (tid < 8) s_rank[n + tid] = 0;
+  if (tid >= n && tid < k) no_choice(p, t, tid);
+  __syncthreads();
   for (int i = tid; i < n; i += kLpThreads) {
     const uint64_t key = s_rank[i];
-    int before = 0;
-    for (int o = 0; o < n; ++o) before += s_rank[o] > key;
+    const int before = keys_above(s_rank, n, key);
     if (before < k) {
       p.top_logprob[t * k + before] = logprob_of(a, key_value((uint32_t)(key >> 32)));
       p.top_id[t * k + before] = (int32_t)~(uint32_t)key;
@@ -541,8 +634,8 @@ __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs_grad_flat(mca_token_
 
 LogprobsPlan lm_logprobs_plan(const mca_token_logprobs_args& a) {
   LogprobsPlan p{1, 0};
-  if (a.n_vocab <= kLpSmall || a.n_rows == 0) return p;
-  const int64_t want = (1024 + a.n_rows - 1) / a.n_rows, most = (a.n_vocab + 8191) / 8192;
+  if (a.n_vocab <= 2 * kLpPart || a.n_rows == 0) return p;
+  const int64_t want = (1024 + a.n_rows - 1) / a.n_rows, most = (a.n_vocab + kLpPart - 1) / kLpPart;
   p.splits = (int32_t)std::clamp<int64_t>(std::min(want, most), 1, kLpSplits);
   if (p.splits > 1) p.bytes = (size_t)a.n_rows * p.splits * (sizeof(uint64_t) * a.n_top + sizeof(Sums));
   return p;

@@ -80,20 +80,28 @@ def test_sizes(lm, typ, vocab):
 @pytest.mark.parametrize("rows", [1, 3, 64, 700])
 def test_row_counts(lm, rows):
     """From a row split over many workgroups to a workgroup a row."""
-    z, tok = make(rows, "bf16", rows, 40001)
-    check(z, tok, lm.mca_token_logprobs(z, tok, 20), 20)
+    for vocab in (40001,) if rows > 3 else (40001, 262144, 262145, 600011):
+        z, tok = make(rows, "bf16", rows, vocab)
+        for n in (0, 20):
+            check(z, tok, lm.mca_token_logprobs(z, tok, n), n)
 
 
-@pytest.mark.parametrize("vocab", [300, 5000, 50000])
+@pytest.mark.parametrize("vocab", [300, 5000, 50000, 300000])
 def test_ties(lm, vocab):
     """Equal values, the two zeros among them: the lowest symbols, in order."""
+    for rows in (4, 600):
+        _ties(lm, vocab, rows)
+
+
+def _ties(lm, vocab, rows):
     rng = np.random.default_rng(vocab)
-    z = torch.from_numpy(rng.integers(-2, 2, (4, vocab)).astype(np.float32)).to(torch.bfloat16).cuda()
+    z = torch.from_numpy(rng.integers(-2, 2, (rows, vocab)).astype(np.float32)).to(torch.bfloat16).cuda()
     z[1] = 0.0
     z[1, ::3] = -0.0
     z[2] = 1.0
-    tok = torch.zeros(4, dtype=torch.int32, device="cuda")
-    check(z, tok, lm.mca_token_logprobs(z, tok, 32), 32)
+    tok = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    res = lm.mca_token_logprobs(z, tok, 32)
+    check(z[:8], tok[:8], [x[:8] for x in res], 32)
 
 
 @pytest.mark.parametrize("typ", ["f32", "bf16"])
@@ -101,9 +109,11 @@ def test_ties(lm, vocab):
 def test_ordered_rows(lm, typ, order):
     """Every chunk (or none) passes the largest so far."""
     z = torch.linspace(-20, 20, 60000)
-    z = (z if order == "rising" else z.flip(0)).to(TYPES[typ]).cuda()[None].repeat(2, 1)
-    tok = torch.tensor([0, 59999], device="cuda")
-    check(z, tok, lm.mca_token_logprobs(z, tok, 32), 32)
+    for rows in (2, 600):
+        y = (z if order == "rising" else z.flip(0)).to(TYPES[typ]).cuda()[None].repeat(rows, 1)
+        tok = torch.arange(rows, device="cuda")
+        res = lm.mca_token_logprobs(y, tok, 32)
+        check(y[:2], tok[:2], [x[:2] for x in res], 32)
 
 
 @pytest.mark.parametrize("vocab", [70, 900, 3001, 80000])
@@ -242,7 +252,7 @@ def test_many_rows(lm):
 
 def test_refusals(lm):
     from paper_2607_08406_amd.mca import MCAError
-    z, tok = make(1, "bf16", 2, 40000)
+    z, tok = make(1, "bf16", 2, 300000)
     for bad in (lambda: lm.mca_token_logprobs(z, tok, 33), lambda: lm.mca_token_logprobs(z.T, tok[:1]),
                 lambda: lm.mca_token_logprobs(z, tok.float()), lambda: lm.mca_token_logprobs(z, tok.cpu()),
                 lambda: lm.mca_token_logprobs(z, tok[:1]), lambda: lm.mca_token_logprobs(z.double(), tok),

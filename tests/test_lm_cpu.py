@@ -111,7 +111,7 @@ def test_tree_attention_refuses(lib, kw, code, word):
     refused(lib, lib.mca_tree_attention(ctypes.byref(a), None), code, word)
 
 
-LOGPROBS = dict(dtype=1, n_top=5, token_bytes=8, n_rows=2, n_vocab=50000, logits_row=50000, logits=P, tokens=P, logprob=P,
+LOGPROBS = dict(dtype=1, n_top=5, token_bytes=8, n_rows=2, n_vocab=500000, logits_row=500000, logits=P, tokens=P, logprob=P,
                 entropy=P, lse=P, top_logprob=P, top_id=P, workspace=P, workspace_bytes=1 << 30)
 
 
@@ -125,7 +125,7 @@ LOGPROBS = dict(dtype=1, n_top=5, token_bytes=8, n_rows=2, n_vocab=50000, logits
     (dict(n_rows=2 ** 24), mca.MCA_EUNSUPPORTED, "rows"),
     (dict(n_vocab=2 ** 30 + 1, logits_row=2 ** 31), mca.MCA_EUNSUPPORTED, "n_vocab"),
     (dict(token_bytes=2), mca.MCA_EINVAL, "token_bytes"),
-    (dict(logits_row=49999), mca.MCA_EINVAL, "logits_row"),
+    (dict(logits_row=499999), mca.MCA_EINVAL, "logits_row"),
     (dict(top_id=None), mca.MCA_EINVAL, "NULL"),
     (dict(logits=P + 1), mca.MCA_EINVAL, "aligned"),
     (dict(tokens=P + 4), mca.MCA_EINVAL, "aligned"),
@@ -188,7 +188,7 @@ def test_plans(lib):
     assert lib.mca_token_logprobs_plan(ctypes.byref(b), ctypes.byref(n)) == 0 and n.value == 0
     b = fill(mca.mca_token_logprobs_args, LOGPROBS, dict())
     assert lib.mca_token_logprobs_plan(ctypes.byref(b), ctypes.byref(n)) == 0 and n.value > 0
-    assert lm.mca_token_logprobs_plan(torch.empty(2, 50000, dtype=torch.bfloat16), 5) == n.value
+    assert lm.mca_token_logprobs_plan(torch.empty(2, 500000, dtype=torch.bfloat16), 5) == n.value
 
 
 def test_tensors_without_a_gpu_are_refused():

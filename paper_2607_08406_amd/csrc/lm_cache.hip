@@ -51,8 +51,7 @@ __global__ __launch_bounds__(kTabThreads) void k_lm_tables(TablesArgs a) {
   const int per = (R + kTabEntries - 1) / kTabEntries;  // requests of an entry
   const int ne = (R + per - 1) / per;
   const int most = a.max_blocks * B;  // below 2^31 (checked on the host)
-  auto change = [&](int r, int* bad) -> Change {
-    const int o = a.old_len[r], n = a.new_len[r];
+  auto change_of = [&](int o, int n, int* bad) -> Change {
     if (o < 0 || o > most || n < 0 || n > most) {
       *bad = 1;
       return {0, 0, 0, 0};
@@ -60,17 +59,36 @@ __global__ __launch_bounds__(kTabThreads) void k_lm_tables(TablesArgs a) {
     const int have = (int)(((unsigned)o + B - 1) / (unsigned)B), want = (int)(((unsigned)n + B - 1) / (unsigned)B);
     return {n > o ? n - o : 0, want > have ? want - have : 0, have > want ? have - want : 0, have};
   };
+  auto change = [&](int r, int* bad) -> Change { return change_of(a.old_len[r], a.new_len[r], bad); };
+  const int pt = (ne + kTabThreads - 1) / kTabThreads;  // entries of a thread
   if (tid == 0) s_bad = 0;
   __syncthreads();
   int bad = 0;
   Change mine{0, 0, 0, 0};
   Change ent[kTabPer];
+  if (per == 1) {
+    // all of a thread's lengths requested before the first is looked at
+    int o[kTabPer], n[kTabPer];
 #pragma unroll
-  for (int u = 0; u < kTabPer; ++u) {
-    const int e = tid * kTabPer + u;
-    ent[u] = {0, 0, 0, 0};
-    for (int r = e * per; r < (e + 1) * per && r < R; ++r) ent[u] = plus(ent[u], change(r, &bad));
-    mine = plus(mine, ent[u]);
+    for (int u = 0; u < kTabPer; ++u) {
+      const int r = min(tid * pt + (u < pt ? u : 0), R - 1);
+      o[u] = gload(a.old_len + r);
+      n[u] = gload(a.new_len + r);
+    }
+#pragma unroll
+    for (int u = 0; u < kTabPer; ++u) {
+      ent[u] = {0, 0, 0, 0};
+      if (u < pt && tid * pt + u < R) ent[u] = change_of(o[u], n[u], &bad);
+      mine = plus(mine, ent[u]);
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < kTabPer; ++u) {
+      const int e = tid * pt + u;
+      ent[u] = {0, 0, 0, 0};
+      for (int r = e * per; u < pt && r < (e + 1) * per && r < R; ++r) ent[u] = plus(ent[u], change(r, &bad));
+      mine = plus(mine, ent[u]);
+    }
   }
   if (bad) s_bad = 1;
   Change run = mine;  // inclusive over the wave's threads
@@ -92,8 +110,8 @@ __global__ __launch_bounds__(kTabThreads) void k_lm_tables(TablesArgs a) {
   }
 #pragma unroll
   for (int u = 0; u < kTabPer; ++u) {
-    const int e = tid * kTabPer + u;
-    if (e < ne) {
+    const int e = tid * pt + u;
+    if (u < pt && e < ne) {
       s_add[e] = before.add;
       s_grow[e] = before.grow;
       s_back[e] = before.back;

@@ -106,7 +106,7 @@ int mca_cache_append(const mca_cache_append_args* args, void* hip_stream);
  * count as the nearest of these; cached tokens behind max_blocks or in a block
  * outside [0, n_blocks) are not there.  lse may be NULL.
  * head_dim at most 256, and head_dim, strides and addresses multiples of 16
- * bytes; n_blocks * n_kv_head * block_size below 2^31.  Scores, softmax and
+ * bytes; max_len at most 2^30, n_blocks * n_kv_head * block_size below 2^31.  Scores, softmax and
  * sums in 32 bits; the weights of 16-bit values are rounded to 16 bits. */
 typedef struct mca_tree_attention_args {
   int32_t dtype, n_req, n_head, n_kv_head, head_dim, block_size, n_blocks, max_blocks, max_nodes,
@@ -192,7 +192,8 @@ int mca_token_logprobs_grad(const mca_token_logprobs_grad_args* args, void* hip_
  * (rows logits_row apart) receives the nodes' logits; rows behind the last
  * request stay as they were there and are unspecified in qkv.  A node whose
  * token is outside the vocabulary or whose position is outside the context
- * gets NaN, and so do the nodes that see it, no others.  On the context's
+ * gets NaN, and so do the nodes that see it, no others.  n_rows times the
+ * widest of 3 d_model, d_mlp and vocabulary below 2^31.  On the context's
  * stream; not synchronised.  MLP contexts: MCA_EINVAL.
  * ------------------------------------------------------------------------ */
 typedef struct mca_extend_args {

@@ -52,7 +52,8 @@ const char* lm_check_attention(const mca_tree_attention_args& a, int* code) {
   *code = MCA_EUNSUPPORTED;
   if (a.head_dim > 256) return "head_dim must be at most 256";
   if (a.head_dim * type_bytes(a.dtype) % 16 != 0) return "head_dim must be a multiple of 16 bytes";
-  if ((int64_t)a.max_blocks * a.block_size > kMaxInt || a.max_len > kMaxInt) return "cached tokens must stay below 2^31 - 1";
+  if ((int64_t)a.max_blocks * a.block_size > kMaxInt) return "max_blocks * block_size must stay below 2^31 - 1";
+  if (a.max_len > (1 << 30)) return "max_len must be at most 2^30";  // positions behind the last fit 32 bits
   if ((int64_t)a.n_blocks * a.n_kv_head > kMaxInt || (int64_t)a.n_blocks * a.n_kv_head * a.block_size > kMaxInt)
     return "n_blocks * n_kv_head * block_size must stay below 2^31 - 1";
   // workgroups: at least 16 rows each, and a few thousand more when split

@@ -564,7 +564,8 @@ __device__ __forceinline__ RowGrad row_grad(const mca_token_logprobs_grad_args& 
   return r;
 }
 __device__ __forceinline__ float grad_of(const RowGrad& r, float z, bool token) {
-  const float lp = fmaxf(z - r.lse, kFar);
+  // a bound below which probabilities are 0: the product with ge stays finite
+  const float lp = fmaxf(z - r.lse, -1e4f);
   // NaN must stay: the maximum drops it from lp, not from the probability
   const float q = __builtin_amdgcn_exp2f((z - r.lse) * kLog2e);
   const float d = -q * fmaf(r.ge, lp + r.entropy, r.g);

@@ -541,7 +541,11 @@ int check_extend(mca_ctx* ctx, const mca_extend_args& x) {
   if (!ctx->tf) return fail(ctx, MCA_EINVAL, "mca_extend takes a Transformer context");
   int code;
   const char* msg = mca::lm_check_attention(mca::tf_extend_attention(ctx->tfh, x), &code);
-  return msg == nullptr ? MCA_OK : fail(ctx, code, msg);
+  if (msg != nullptr) return fail(ctx, code, msg);
+  const mca::TfDev& h = ctx->tfh;  // the widest of a row's activations
+  if ((int64_t)x.n_rows * std::max({3 * h.D, h.M, h.V}) > INT32_MAX)
+    return fail(ctx, MCA_EUNSUPPORTED, "n_rows times the net's widest activation must stay below 2^31");
+  return MCA_OK;
 }
 
 // Waits for a step loop's stream by polling it for up to a millisecond, then

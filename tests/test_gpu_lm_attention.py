@@ -128,6 +128,45 @@ def test_many_rows_share_a_key_head(lm, typ):
     check(s, call(lm, s))
 
 
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("dim", [32, 64, 80, 128, 200, 256])
+@pytest.mark.parametrize("group,nodes", [(1, 40), (4, 13), (8, 20)])
+def test_shared_work(lm, typ, dim, group, nodes):
+    """Many rows over long and short contexts: the workgroups' shares begin and end inside requests, key heads, tiles
+    of rows and drafted tiles."""
+    s = make(dim + nodes, typ, [0, 2300, 70, 2049, 1], [nodes, max(1, nodes - 5), 0, nodes, 3], 2 * group, 2, dim, 16)
+    a = call(lm, s)
+    check(s, a)
+    b = call(lm, s)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+def test_shared_work_of_many_requests(lm, typ):
+    """More requests than a workgroup has threads, most of them short or without nodes."""
+    rng = np.random.default_rng(3)
+    lens = rng.integers(0, 40, 700)
+    lens[[5, 300, 699]] = [2500, 1200, 3000]
+    nodes = np.where(rng.random(700) < 0.8, 0, rng.integers(1, 3, 700))
+    nodes[[5, 300, 699]] = [40, 3, 33]
+    s = make(61, typ, list(lens), list(nodes), 1, 1, 32, 16)
+    check(s, call(lm, s))
+
+
+def test_shared_work_with_bad_blocks_and_values(lm):
+    """Blocks that are not there inside whole tiles, and drafted values that are not finite, at every place of a share."""
+    s = make(67, "bf16", [2500, 1500], [60, 37], 4, 2, 64, 16)
+    for r, c in ((0, 3), (0, 70), (0, 71), (0, 155), (1, 0), (1, 93)):
+        s["table"][r, c] = -1
+    s["parents"][:60] = torch.arange(-1, 59, dtype=torch.int32, device="cuda")
+    s["parents"][50:60] = 20
+    s["v"][40] = float("nan")  # nodes 40 to 49 see it
+    s["k"][51], s["v"][51] = float("inf"), float("nan")  # node 51 alone
+    out, lse = call(lm, s)
+    check(s, (out, lse), skip=[51])
+    assert torch.isnan(out[40:50]).all() and torch.isfinite(out[:40]).all() and torch.isfinite(out[52:97]).all()
+
+
 def test_ragged_and_empty_requests(lm):
     """Requests without nodes between others, and rows behind the last request left as they were."""
     s = make(13, "bf16", [9, 50, 0, 18, 400], [2, 0, 3, 0, 1], 4, 4, 64, 16)

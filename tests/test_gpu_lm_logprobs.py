@@ -223,6 +223,22 @@ def test_gradient(lm, typ, vocab):
     check_grad(z, tok, res.lse, res.entropy, g, ge, mine)
 
 
+@pytest.mark.parametrize("vocab", [70, 5001])
+@pytest.mark.parametrize("typ", ["f32", "bf16"])
+def test_large_gradients_of_masked_symbols(lm, typ, vocab):
+    """Symbols of probability 0 get 0, however large the gradient of the entropy is."""
+    z, tok = make(vocab + 1, typ, 5, vocab)
+    z[:, 3::2] = -float("inf")
+    z[:, 2] = -3e4
+    tok[:] = 0
+    res = lm.mca_token_logprobs(z, tok)
+    g, ge = torch.randn(2, 5, device="cuda")
+    ge = ge * 1e12
+    got = lm.mca_token_logprobs_grad(z, tok, res.lse, res.entropy, g, ge)
+    assert (got[:, 2:4] == 0).all()
+    check_grad(z, tok, res.lse, res.entropy, g, ge, got)
+
+
 def test_gradient_against_differences(lm):
     z, tok = make(5, "f32", 2, 1200)
     g, ge = torch.randn(2, 2, device="cuda")

@@ -191,6 +191,18 @@ def test_refusals(lm):
     ctx.close()
 
 
+def test_extend_refuses_more_rows_than_it_can_address(lm):
+    from paper_2607_08406_amd import mca
+    ctx, cfg, _ = make(ctx=32, d_model=64, n_head=2, n_seq=2, d_mlp=96)
+    lib, room = mca.load_library(), ctypes.c_size_t()
+    a = mca.mca_extend_args(n_req=1, n_rows=2 ** 31 // (3 * 64) + 1, max_nodes=1, max_len=32, block_size=8, n_blocks=4, max_blocks=4)
+    assert lib.mca_extend_plan(ctx.ctx, ctypes.byref(a), ctypes.byref(room)) == mca.MCA_EUNSUPPORTED
+    assert lib.mca_extend(ctx.ctx, ctypes.byref(a)) == mca.MCA_EUNSUPPORTED
+    a.n_rows -= 1
+    assert lib.mca_extend_plan(ctx.ctx, ctypes.byref(a), ctypes.byref(room)) == mca.MCA_OK
+    ctx.close()
+
+
 def test_captured_step(lm):
     """Tables, net, rows and log probabilities in one graph; each replay on new inputs equals the eager calls, with
     eager work and other graphs' replays in between."""

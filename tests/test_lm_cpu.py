@@ -92,6 +92,8 @@ ATTENTION = dict(dtype=1, n_req=3, n_head=8, n_kv_head=2, head_dim=64, block_siz
     (dict(max_nodes=0), mca.MCA_EINVAL, "max_nodes"),
     (dict(max_nodes=129), mca.MCA_EINVAL, "max_nodes"),
     (dict(max_len=-1), mca.MCA_EINVAL, "max_len"),
+    (dict(max_len=2 ** 30 + 1), mca.MCA_EUNSUPPORTED, "2^30"),
+    (dict(max_blocks=2 ** 27, table_stride=2 ** 27), mca.MCA_EUNSUPPORTED, "2^31"),
     (dict(block_size=0), mca.MCA_EINVAL, "positive"),
     (dict(n_blocks=2 ** 27, block_size=16), mca.MCA_EUNSUPPORTED, "2^31"),
     (dict(n_req=65535, max_nodes=128, n_head=64, n_kv_head=2), mca.MCA_EUNSUPPORTED, "too many"),

@@ -16,6 +16,8 @@ from oracle import lm as olm
 
 pytestmark = pytest.mark.gpu
 
+LONG = 1 << 17  # a max_len at which many rows are worked on in shares
+
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 
 
@@ -129,15 +131,27 @@ def test_many_rows_share_a_key_head(lm, typ):
 
 
 @pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("dim", [32, 96, 128, 136, 256])
+@pytest.mark.parametrize("rows", [17, 32, 33, 64, 65, 128, 224, 256, 257])
+@pytest.mark.parametrize("more", [0, 600])
+def test_rows_of_a_key_head(lm, typ, dim, rows, more):
+    """Numbers of rows around those at which waves and workgroups take more; contexts of few tiles.  With many
+    requests (which are empty) a tile is read once for many rows."""
+    group, nodes = (1, rows) if rows < 100 else ((2, rows // 2) if rows % 2 == 0 else (257, 1))
+    s = make(rows, typ, [200, 33, 0] + [0] * more, [nodes, max(1, nodes // 3), 1] + [0] * more, group, 1, dim, 16)
+    check(s, call(lm, s))
+
+
+@pytest.mark.parametrize("typ", ["f32", "bf16", "f16"])
 @pytest.mark.parametrize("dim", [32, 64, 80, 128, 200, 256])
-@pytest.mark.parametrize("group,nodes", [(1, 40), (4, 13), (8, 20)])
+@pytest.mark.parametrize("group,nodes", [(1, 40), (4, 13), (8, 20), (8, 30)])
 def test_shared_work(lm, typ, dim, group, nodes):
     """Many rows over long and short contexts: the workgroups' shares begin and end inside requests, key heads, tiles
     of rows and drafted tiles."""
     s = make(dim + nodes, typ, [0, 2300, 70, 2049, 1], [nodes, max(1, nodes - 5), 0, nodes, 3], 2 * group, 2, dim, 16)
-    a = call(lm, s)
+    a = call(lm, s, max_len=LONG)
     check(s, a)
-    b = call(lm, s)
+    b = call(lm, s, max_len=LONG)
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
@@ -150,7 +164,7 @@ def test_shared_work_of_many_requests(lm, typ):
     nodes = np.where(rng.random(700) < 0.8, 0, rng.integers(1, 3, 700))
     nodes[[5, 300, 699]] = [40, 3, 33]
     s = make(61, typ, list(lens), list(nodes), 1, 1, 32, 16)
-    check(s, call(lm, s))
+    check(s, call(lm, s, max_len=LONG))
 
 
 def test_shared_work_with_bad_blocks_and_values(lm):
@@ -162,9 +176,15 @@ def test_shared_work_with_bad_blocks_and_values(lm):
     s["parents"][50:60] = 20
     s["v"][40] = float("nan")  # nodes 40 to 49 see it
     s["k"][51], s["v"][51] = float("inf"), float("nan")  # node 51 alone
-    out, lse = call(lm, s)
+    out, lse = call(lm, s, max_len=LONG)
     check(s, (out, lse), skip=[51])
     assert torch.isnan(out[40:50]).all() and torch.isfinite(out[:40]).all() and torch.isfinite(out[52:97]).all()
+
+
+@pytest.mark.parametrize("typ,dim", [("bf16", 64), ("f16", 128), ("bf16", 256), ("f32", 128), ("f32", 64)])
+def test_single_tokens_over_long_contexts_in_plenty(lm, typ, dim):
+    s = make(71, typ, [2300, 0, 70, 3000, 16, 1], [1, 2, 1, 0, 4, 1], 8, 2, dim, 16)
+    check(s, call(lm, s, max_len=1 << 20))
 
 
 def test_ragged_and_empty_requests(lm):

@@ -168,6 +168,15 @@ def test_calls_without_rows_enqueue_nothing(lib):
         assert call(ctypes.byref(a), None) == mca.MCA_OK
 
 
+def test_plans_without_requests_or_rows(lib):
+    n = ctypes.c_size_t(7)
+    for kw in (dict(n_req=0), dict(n_req=0, max_nodes=128), dict(n_rows=0), dict(max_len=0, max_blocks=0)):
+        a = fill(mca.mca_tree_attention_args, ATTENTION, kw)
+        assert lib.mca_tree_attention_plan(ctypes.byref(a), ctypes.byref(n)) == mca.MCA_OK
+    a = fill(mca.mca_token_logprobs_args, LOGPROBS, dict(n_rows=0))
+    assert lib.mca_token_logprobs_plan(ctypes.byref(a), ctypes.byref(n)) == mca.MCA_OK and n.value == 0
+
+
 def test_null_arguments(lib):
     n = ctypes.c_size_t()
     for call, args in [(lib.mca_cache_append, (None, None)), (lib.mca_tree_attention, (None, None)),

@@ -104,8 +104,9 @@ __device__ __forceinline__ int chunks_of(int len, int chunk) { return max(1, (le
 // 16 + 4 q + j - 4.  V comes in as rows: a lane has the same few dimensions of
 // its 8 tokens, so 16 lanes read a whole row, and pairs of tokens are put
 // together by one byte permutation per word; the result's row li then is
-// dimension li * (dimensions of a lane) + e.  fp32 takes v_mfma_f32_16x16x4f32
-// with one token of a lane a step.
+// dimension li * (dimensions of a lane) + e.  So no score and no value passes through
+// LDS to change its layout.  fp32 takes v_mfma_f32_16x16x4f32 with one token of a
+// lane a step.
 //
 // DP is head_dim rounded up; with PAD the missing dimensions are zero.
 template <int TYPE, int DP, int QT, int NH, bool PAD>
@@ -182,7 +183,10 @@ struct Rows {
     }
   }
   // weights of the tile; see[t][h] has a bit for each token of the h-th 32 that
-  // query t sees, all of them if `every`
+  // query t sees, all of them if `every`.  The 16-bit types' weights are rounded to
+  // 16 bits, as their products take them; the sum takes them in 32.  A result is off by
+  // half a step of the weights' share of sum p |v| for that, no more than by its own
+  // rounding; fp32 weights would cost the products at a sixteenth of the rate.
   __device__ __forceinline__ void weigh(bool every, const uint32_t (&see)[QT][NH]) {
     if (!every) {
 #pragma unroll
@@ -472,6 +476,12 @@ struct Share {
 // into registers, each with a running maximum, sum and result of its own, which are
 // joined in LDS at the end, and chunks in a second launch.  The last chunk's
 // workgroup also takes the drafted tokens, each wave 32 nodes.
+//
+// Bound by memory where there is enough to read: a cached value is read once and
+// used 16 times, and nothing is shared between the waves that LDS would save (200
+// requests of 1000 to 2000, one row a head, 4 key heads of 128, bf16: 0.6 GB in
+// 131 us).  Small calls are bound by the chain of table entry, K, scores, V (64 drafts
+// of up to 8 nodes over at most 120 tokens, 4 heads of 32, fp32: 8.5 us).
 template <int TYPE, int DP, bool PAD>
 __global__ __launch_bounds__(kAttnThreads) void k_lm_attn(AttnDev p) {
   typedef Rows<TYPE, DP, 1, 1, PAD> R;
@@ -593,6 +603,15 @@ __global__ __launch_bounds__(kAttnThreads) void k_lm_attn(AttnDev p) {
 // requested while the one before is worked on, and stored behind it, with one
 // barrier a tile.  A row's 16-byte parts change places with the row, so that the
 // 16 lanes that read one part of 16 rows take all 64 banks.
+//
+// Bound by the matrix and vector units together: a 16-bit score takes head_dim / 256
+// cycles of a SIMD's matrix core over both products and about 8 vector instructions
+// (maximum, exponential, sum, packing) of a sixteenth of a cycle, which only another
+// wave's products hide.  16 requests of 4096 to 16384, 192 to 384 rows, 4 key heads of 128,
+// fp16 (95 GFLOP): 255 us and 26 of joining, 340 TFLOP/s of the 1217 that a large
+// product reaches; at 256 rows in each, 16384: 750.  One request of 262144, 96 rows,
+// 2 key heads of 64, bf16 (134 MB): 41 and 10.  16 rows of a wave, 32 requests of 8192
+// to 32768, one row a head, 8 key heads of 128, bf16 (2.63 GB): 465 and 8, 5.6 TB/s.
 template <int TYPE, int DP, int QT, int NW, bool PAD>
 __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 ? 1 : 2) void k_lm_attn_wide(AttnDev) {
   constexpr int EL = TYPE == MCA_TYPE_F32 ? 4 : 2;
@@ -922,14 +941,14 @@ __global__ __launch_bounds__(256) void k_lm_attn_join(AttnDev p) {
 
 // The parts of shared work joined: a workgroup takes 4 `fours` rows of one tile of
 // rows, which are cut in the same places, 4 at a time: their weights are made in
-// LDS, then its 4 waves take parts in turn and are added there.  head_dim is at
+// LDS, then its NW waves take parts in turn and are added there.  head_dim is at
 // most 64 NI.
 constexpr int kMaxSharers = 512;
-template <int TYPE, int NI>
-__global__ __launch_bounds__(256) void k_lm_attn_join_shared(AttnDev p, int TP, int fours) {
+template <int TYPE, int NI, int NW>
+__global__ __launch_bounds__(64 * NW) void k_lm_attn_join_shared(AttnDev p, int TP, int fours) {
   const mca_tree_attention_args& a = p.a;
   __shared__ float s_w[4][kMaxSharers];
-  __shared__ float s_acc[4][4 * 64 * NI];
+  __shared__ float s_acc[NW][4 * 64 * NI];
   const int groups = p.rows / (4 * fours), tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int tile = blockIdx.x / groups, rt = tile % p.row_tiles, rh = tile / p.row_tiles;
   const int h = rh % a.n_kv_head, r = rh / a.n_kv_head;
@@ -948,7 +967,7 @@ __global__ __launch_bounds__(256) void k_lm_attn_join_shared(AttnDev p, int TP, 
   auto at = [&](int s) { return (int64_t)(2 * (g0 + s) + (s == 0 ? late : 0)) * p.rows + row0; };
   const int D = a.head_dim, all = 4 * D;  // a multiple of 16
   for (int four = 0; four < fours && row0 < rows; ++four, row0 += 4) {
-    {
+    if (wave < 4) {
       const bool here = row0 + wave < rows;
       float top = -__builtin_huge_valf(), sum = 0.f;
       for (int s = lane; s < parts; s += 64) {
@@ -985,7 +1004,7 @@ __global__ __launch_bounds__(256) void k_lm_attn_join_shared(AttnDev p, int TP, 
       of_e[i] = at_e[i] / D;
     }
 #pragma unroll 8
-    for (int s = wave; s < parts; s += 4) {
+    for (int s = wave; s < parts; s += NW) {
       const float* po = p.part_o + at(s) * D;
 #pragma unroll
       for (int i = 0; i < NI; ++i) acc[i] += s_w[of_e[i]][s] * gload((const f32x4*)(po + at_e[i]));
@@ -994,10 +1013,12 @@ __global__ __launch_bounds__(256) void k_lm_attn_join_shared(AttnDev p, int TP, 
     for (int i = 0; i < NI; ++i)
       if (4 * (lane + 64 * i) < all) *(f32x4*)&s_acc[wave][at_e[i]] = acc[i];
     __syncthreads();
-    for (int e = tid; e < all; e += 256) {
+    for (int e = tid; e < all; e += 64 * NW) {
       const int of = e / D, row = rt * sh.rows + row0 + of, node = row / p.group;
       if (row0 + of >= rows) break;
-      const float x = (s_acc[0][e] + s_acc[1][e]) + (s_acc[2][e] + s_acc[3][e]);
+      float x = s_acc[0][e];
+#pragma unroll
+      for (int u = 1; u < NW; ++u) x += s_acc[u][e];
       const int64_t to = (int64_t)(first + node) * a.out_row + (int64_t)(h * p.group + (row - node * p.group)) * a.out_head + (e - of * D);
       if constexpr (TYPE == MCA_TYPE_F32)
         ((float*)a.out)[to] = x;
@@ -1088,6 +1109,17 @@ void launch_dim(const AttnDev& p, dim3 grid, hipStream_t s) {
   else
     launch_pad<TYPE, DP, true>(p, grid, s);
 }
+// 16 waves of a workgroup where there are few, each with many parts to read, else 4
+// (with the attention, 16 and 4 waves: one request of 60000, 64 rows, 4 key heads, bf16,
+// head_dim 128, 64 workgroups, 48 and 51 us, head_dim 256 89 and 115; 4 requests of
+// 8192, 128 rows, head_dim 128, 512 workgroups, 58 and 54).
+template <int TYPE, int NI>
+void launch_join(const AttnDev& p, dim3 groups, int fours, hipStream_t s) {
+  if (groups.x <= kCUs)
+    hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 16>), groups, dim3(1024), 0, s, p, tile_tokens(p.a), fours);
+  else
+    hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 4>), groups, dim3(256), 0, s, p, tile_tokens(p.a), fours);
+}
 template <int TYPE>
 void launch_type(const AttnDev& p, dim3 grid, hipStream_t s) {
   const int D = p.a.head_dim;
@@ -1109,11 +1141,11 @@ void launch_type(const AttnDev& p, dim3 grid, hipStream_t s) {
     const int fours = wide_items(p.a) * p.rows / 16 >= 4 * kCUs ? 4 : 1;
     const dim3 groups((unsigned)(wide_items(p.a) * (p.rows / (4 * fours))));
     if (D <= 64)
-      hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, 1>), groups, dim3(256), 0, s, p, tile_tokens(p.a), fours);
+      launch_join<TYPE, 1>(p, groups, fours, s);
     else if (D <= 128)
-      hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, 2>), groups, dim3(256), 0, s, p, tile_tokens(p.a), fours);
+      launch_join<TYPE, 2>(p, groups, fours, s);
     else
-      hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, 4>), groups, dim3(256), 0, s, p, tile_tokens(p.a), fours);
+      launch_join<TYPE, 4>(p, groups, fours, s);
   }
 }
 

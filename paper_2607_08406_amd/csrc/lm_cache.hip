@@ -42,6 +42,10 @@ __device__ __forceinline__ Change plus(const Change& a, const Change& b) {
 //
 // Sums saturate at 2^31 - 1, above every limit they are compared with
 // (max_tokens and n_blocks are at most 2^31 - 2).
+//
+// Bound by latency: lengths, two barriers of sums, then a search in LDS and a chain of
+// two loads for an item.  256 decoding requests: 9.4 us, 4001 of a serving step with
+// room for 924 thousand slots 26 us.
 __global__ __launch_bounds__(kTabThreads) void k_lm_tables(TablesArgs a) {
   __shared__ int s_add[kTabEntries + 1], s_grow[kTabEntries + 1], s_back[kTabEntries + 1];
   __shared__ Change s_wave[kTabThreads / 64];
@@ -224,7 +228,9 @@ hipError_t lm_launch_tables(const TablesArgs& a, hipStream_t s) {
 
 // Copies units of sizeof(U) bytes: a row has n_kv_head * per_head of them in K
 // and as many in V.  A workgroup takes rows_per_group rows.  Bound by memory: a
-// thread has kAppendUnits units of K and of V in flight.
+// thread has kAppendUnits units of K and of V in flight.  65000 rows of 8 heads of 128,
+// bf16 (533 MB read and written): 104 us, 5.1 TB/s; 256 rows of 4 heads of 32, fp32: 5.5
+// us.  Units of 4 and of 2 bytes are for heads and strides that are no multiples of 16.
 template <class U>
 __global__ __launch_bounds__(kAppendThreads) void k_lm_append(mca_cache_append_args a, int per_head, int scale,
                                                               int rows_per_group) {

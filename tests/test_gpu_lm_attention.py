@@ -302,6 +302,22 @@ def test_rows_behind_32_bit_offsets(lm):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def test_many_rows_behind_32_bit_offsets(lm):
+    dim, block, kv = 128, 64, 8
+    n_blocks = (2 ** 32 // (dim * 2 * block * kv)) + 40
+    s = make(73, "bf16", [1000], [40], 8, kv, dim, block)
+    held = s["k_cache"].shape[0]
+    small = dict(s)
+    for n in ("k_cache", "v_cache"):
+        big = torch.zeros(n_blocks, kv, block, dim, dtype=torch.bfloat16, device="cuda")
+        big[n_blocks - held:] = s[n]
+        s[n] = big
+    s["table"] = s["table"] + (n_blocks - held)
+    want, got = call(lm, small, max_len=LONG), call(lm, s, max_len=LONG)
+    check(small, want)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_refusals(lm):
     from paper_2607_08406_amd.mca import MCAError
     s = make(53, "bf16", [20], [2], 4, 2, 64, 16)

@@ -107,7 +107,8 @@ int mca_cache_append(const mca_cache_append_args* args, void* hip_stream);
  * outside [0, n_blocks) are not there.  lse may be NULL.
  * head_dim at most 256, and head_dim, strides and addresses multiples of 16
  * bytes; max_len at most 2^30, n_blocks * n_kv_head * block_size below 2^31.  Scores, softmax and
- * sums in 32 bits; the weights of 16-bit values are rounded to 16 bits. */
+ * sums in 32 bits; the weights of 16-bit values are rounded to 16 bits, each by at most half a step
+ * of its own or, of fp16, 2^-17 of the largest weight among the 64 tokens around it. */
 typedef struct mca_tree_attention_args {
   int32_t dtype, n_req, n_head, n_kv_head, head_dim, block_size, n_blocks, max_blocks, max_nodes,
       max_len;

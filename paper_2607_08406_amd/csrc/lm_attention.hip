@@ -26,10 +26,27 @@ constexpr int kMaskWords = MCA_MAX_NODES / 32;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-// The running maximum follows the scores only when one passes it by more than
-// this (in powers of two): weights then reach 2^8 at most, which fp16 holds, and
-// the sums of the products are rescaled a few times in all, not once a tile.
-constexpr float kSlack = 8.0f;
+// Weights are powers of two relative to a reference that follows a row's scores only
+// where a tile's largest leaves a window around it, so that the sums of the products
+// are rescaled a few times in all, not once a tile.  With 8 exponent bits (fp32, bf16)
+// the reference is the running maximum and follows what passes it by more than 2^8:
+// smaller weights lose nothing until they are 2^-126.
+//
+// fp16 holds 2^-14 to 2^15 in full and steps of 2^-24 below, while the tokens that
+// make the result may all lie far below the largest weight (a first token that takes
+// nearly all weight and whose value is 0).  So the reference goes down as well: a
+// tile's largest weight is put at 2^11 and stays between 2^-8 and 2^15.  A weight then
+// is off by half a step of its own, or by 2^-25 where it is below 2^-14; over a tile
+// of 64 tokens the latter is 2^-11 of the tile's largest weight at the most, and
+// 2^-29 of it in a tile that has moved the reference.  The reference moves by whole
+// powers, which round nothing, and not below what leaves the sums under 2^80: tokens
+// that lie further down weigh less than 2^-69 of their row's together.  (The second
+// comparison costs 1 %: 16 drafts of 48, 192 to 384 rows, head_dim 128, 276 us against 273.)
+template <int TYPE>
+struct Window {
+  static constexpr bool kMoves = TYPE == MCA_TYPE_F16;
+  static constexpr float kAbove = kMoves ? 15.0f : 8.0f, kBelow = 8.0f, kPut = 11.0f, kMost = 0x1p80f;
+};
 // Units of a workgroup that shares the work: fewer are not worth the joining.  (One
 // request of 4096 tokens, 128 rows a key head, 4 of them, bf16, head_dim 128: 33 us
 // with 2, 35 with 4, 54 with 16; 16 requests of 16384: 138, 136 and 139 us.)
@@ -123,7 +140,8 @@ struct Rows {
   int q, li, first, n, dbytes;
   int node[QT], head[QT];
   u32x4 qf[QT][KL];
-  float m[QT], l[QT], c2;  // maximum times c2 and sum of exponentials so far
+  typedef Window<TYPE> W;
+  float m[QT], l[QT], c2;  // reference of the weights (scores times c2) and their sum so far
   f32x4 o[QT][OT];
   f32x4 s[QT][2 * NH];     // a tile's scores
   // and its weights: 16-bit ones in pairs, as operands of their products
@@ -185,8 +203,8 @@ struct Rows {
   // weights of the tile; see[t][h] has a bit for each token of the h-th 32 that
   // query t sees, all of them if `every`.  The 16-bit types' weights are rounded to
   // 16 bits, as their products take them; the sum takes them in 32.  A result is off by
-  // half a step of the weights' share of sum p |v| for that, no more than by its own
-  // rounding; fp32 weights would cost the products at a sixteenth of the rate.
+  // half a step of sum p |v| for that, and fp16's by what Window says; fp32 weights
+  // would cost the products at a sixteenth of the rate.
   __device__ __forceinline__ void weigh(bool every, const uint32_t (&see)[QT][NH]) {
     if (!every) {
 #pragma unroll
@@ -207,14 +225,24 @@ struct Rows {
 #pragma unroll
         for (int v = 0; v < 4; ++v) top[t] = fmaxf(top[t], s[t][x][v]);
       top[t] *= c2;
-      over = over || top[t] > m[t] + kSlack;
+      over = over || top[t] > m[t] + W::kAbove;
+      if constexpr (W::kMoves) over = over || top[t] < m[t] - W::kBelow;
     }
     if (__ballot(over) != 0) {
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
         top[t] = fmaxf(top[t], __shfl_xor(top[t], 16, 64));
         top[t] = fmaxf(top[t], __shfl_xor(top[t], 32, 64));
-        const float mn = fmaxf(m[t], top[t]), f = __builtin_amdgcn_exp2f(m[t] - mn);
+        float mn = fmaxf(m[t], top[t]);
+        if constexpr (W::kMoves) {
+          const float put = ceilf(top[t]) - W::kPut;
+          float sum = l[t] + __shfl_xor(l[t], 16, 64);
+          sum += __shfl_xor(sum, 32, 64);
+          // (not so if nothing is seen or a score is NaN)
+          const bool down = top[t] < m[t] - W::kBelow && sum * __builtin_amdgcn_exp2f(m[t] - put) <= W::kMost;
+          mn = down || top[t] > m[t] + W::kAbove ? put : m[t];
+        }
+        const float f = __builtin_amdgcn_exp2f(m[t] - mn);
         m[t] = mn;
         l[t] *= f;
 #pragma unroll
@@ -473,7 +501,7 @@ struct Share {
 
 // Few rows: a workgroup takes 16 rows of one request and key head against one
 // chunk of the cached tokens; its 4 waves take tiles in turn, straight from memory
-// into registers, each with a running maximum, sum and result of its own, which are
+// into registers, each with a reference, sum and result of its own, which are
 // joined in LDS at the end, and chunks in a second launch.  The last chunk's
 // workgroup also takes the drafted tokens, each wave 32 nodes.
 //

@@ -100,7 +100,8 @@ int mca_cache_append(const mca_cache_append_args* args, void* hip_stream);
  *   out = softmax(scale * q K^T) V,  lse = log sum exp(scale * q K^T)
  * over those, head h with key head h / (n_head / n_kv_head).  One node is a
  * decoding step; a chain (parents i - 1) is a piece of a prompt.  A value that
- * a node does not see never reaches its result, not if it is infinite or NaN.
+ * a node does not see never reaches its result, not if it is infinite or NaN; a
+ * row of which every score is -inf is NaN, its lse too.
  * Rows behind the last request, and requests of more than max_nodes or of
  * offsets out of range, are left as they were.  lengths outside [0, max_len]
  * count as the nearest of these; cached tokens behind max_blocks or in a block

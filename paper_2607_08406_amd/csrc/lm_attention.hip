@@ -367,10 +367,12 @@ struct Rows {
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       if (node[t] >= n) continue;
-      // a chunk without a token that is there weighs nothing
+      // A part that no weight falls to (none of its tokens is there, or every score is
+      // -inf) weighs nothing.  A whole row sees itself: it has no weights only if every
+      // score is -inf, and then softmax has no value, as the parts joined have none.
       const bool none = l[t] == 0.f;
-      const float inv = none ? 0.f : 1.0f / l[t];
-      const float lse2 = none ? -__builtin_huge_valf() : m[t] + __builtin_amdgcn_logf(l[t]);
+      const float inv = none && !whole ? 0.f : 1.0f / l[t];
+      const float lse2 = none ? (whole ? __builtin_nanf("") : -__builtin_huge_valf()) : m[t] + __builtin_amdgcn_logf(l[t]);
       const int64_t out_row = (int64_t)(first + node[t]);
       if (!whole) {
         const int64_t at = part(t);

@@ -574,11 +574,12 @@ __device__ __forceinline__ RowGrad row_grad(const mca_token_logprobs_grad_args& 
   return r;
 }
 __device__ __forceinline__ float grad_of(const RowGrad& r, float z, bool token) {
-  // a bound below which probabilities are 0: the product with ge stays finite
+  // a bound below which probabilities are 0, so that 0 times the logarithm is 0
   const float lp = fmaxf(z - r.lse, -1e4f);
   // NaN must stay: the maximum drops it from lp, not from the probability
   const float q = __builtin_amdgcn_exp2f((z - r.lse) * kLog2e);
-  const float d = -q * fmaf(r.ge, lp + r.entropy, r.g);
+  // q first: a probability of 0 gives 0 whatever finite number ge is
+  const float d = -fmaf(q * (lp + r.entropy), r.ge, q * r.g);
   return token ? d + r.g : d;
 }
 

@@ -351,19 +351,25 @@ def mca_extend(ctx: "mca.TransformerContext", tokens, parents, offsets, lengths,
 
     The work goes on the context's stream: tensors of another stream are the caller's to order.
     """
-    dev, desc = ctx.device, ctx.desc
+    # the context's own device: its name may lack the index
+    dev, desc = ctx.workspace.device, ctx.desc
+    given = dict(tokens=tokens, parents=parents, offsets=offsets, lengths=lengths, table=table, k_cache=k_cache,
+                 v_cache=v_cache, qkv=qkv, logits=logits)
+    for what, t in given.items():
+        if t is not None and t.device != dev:
+            _refuse(f"{what} is on {t.device}, not {dev}")
     n = tokens.numel()
     with torch.cuda.device(dev), torch.cuda.stream(ctx.stream):
         if qkv is None:
             qkv = torch.empty((desc.n_block, n, 3, desc.n_head, 32), dtype=torch.float32, device=dev)
         if logits is None:
             logits = torch.zeros((n, desc.vocab), dtype=torch.float32, device=dev)
-        a = _extend_args(qkv.device, desc, tokens, parents, offsets, lengths, table, k_cache, v_cache, max_nodes,
-                         max_len, qkv, logits)
+        a = _extend_args(dev, desc, tokens, parents, offsets, lengths, table, k_cache, v_cache, max_nodes, max_len, qkv,
+                         logits)
         lib = load_library()
         nbytes = ctypes.c_size_t(0)
         _check(lib.mca_extend_plan(ctx.ctx, ctypes.byref(a), ctypes.byref(nbytes)), ctx.ctx)
-        room = _room(qkv.device, nbytes.value, workspace)
+        room = _room(dev, nbytes.value, workspace)
         a.workspace, a.workspace_bytes = room.data_ptr(), room.numel()
         _check(lib.mca_extend(ctx.ctx, ctypes.byref(a)), ctx.ctx)
     return logits, qkv

@@ -349,7 +349,8 @@ def mca_extend(ctx: "mca.TransformerContext", tokens, parents, offsets, lengths,
                max_len: Optional[int] = None, qkv=None, logits=None, workspace=None):
     """The context's committed net on drafted nodes; returns (logits [n_rows, vocab], qkv [n_block, n_rows, 3, n_head, 32]).
 
-    The work goes on the context's stream: tensors of another stream are the caller's to order.
+    The work goes on the context's stream.  Where that is not the current one, the caller orders the two (inputs
+    before the call, results after it); the memory of the tensors stays theirs until both streams are done with it.
     """
     # the context's own device: its name may lack the index
     dev, desc = ctx.workspace.device, ctx.desc
@@ -358,7 +359,7 @@ def mca_extend(ctx: "mca.TransformerContext", tokens, parents, offsets, lengths,
     for what, t in given.items():
         if t is not None and t.device != dev:
             _refuse(f"{what} is on {t.device}, not {dev}")
-    n = tokens.numel()
+    n, caller = tokens.numel(), torch.cuda.current_stream(dev)
     with torch.cuda.device(dev), torch.cuda.stream(ctx.stream):
         if qkv is None:
             qkv = torch.empty((desc.n_block, n, 3, desc.n_head, 32), dtype=torch.float32, device=dev)
@@ -372,4 +373,13 @@ def mca_extend(ctx: "mca.TransformerContext", tokens, parents, offsets, lengths,
         room = _room(dev, nbytes.value, workspace)
         a.workspace, a.workspace_bytes = room.data_ptr(), room.numel()
         _check(lib.mca_extend(ctx.ctx, ctypes.byref(a)), ctx.ctx)
+    if caller != ctx.stream:
+        for t in given.values():
+            if t is not None:
+                t.record_stream(ctx.stream)
+        if workspace is not None:
+            workspace.record_stream(ctx.stream)
+        for what, t in (("qkv", qkv), ("logits", logits)):
+            if given[what] is None:
+                t.record_stream(caller)
     return logits, qkv

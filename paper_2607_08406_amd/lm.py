@@ -4,7 +4,9 @@ argument marshalling only.
 Tensors pass as they are: their strides go to the library, and what it does not
 take is refused, not copied.  The work goes on the current stream of the tensors'
 device, and workspaces come from PyTorch's allocator on that stream unless one is
-given.  Nothing is synchronised.
+given.  Nothing is synchronised.  No call records a graph for autograd: while
+gradients are recorded, tensors that require one are refused; given tensors that a
+call writes count as changed in place.
 """
 from __future__ import annotations
 
@@ -12,7 +14,8 @@ import ctypes
 from typing import NamedTuple, Optional
 
 import torch
-from torch._C import _cuda_getCurrentRawStream as _raw_stream
+from torch import is_grad_enabled
+from torch._C import _cuda_getCurrentRawStream as _raw_stream, _increment_version as increment_version
 
 from . import mca
 from .mca import (MCA_EDEVICE, MCA_EINVAL, MCAError, _check, load_library, mca_cache_append_args, mca_extend_args,
@@ -73,6 +76,11 @@ def _whole(device, dtype, what, t, shape):
         _refuse(f"{what} is not a contiguous tensor of shape {tuple(shape)}")
 
 
+def _no_graph(**tensors):
+    what = next(what for what, t in tensors.items() if t is not None and t.requires_grad)
+    _refuse(f"{what} requires grad, but the call records no graph: detach it, or call under torch.no_grad()")
+
+
 def _gpu(t: torch.Tensor) -> torch.device:
     if not t.is_cuda:
         raise MCAError(MCA_EDEVICE, f"a tensor on {t.device}: the operators run only on the GPU")
@@ -117,11 +125,14 @@ def mca_block_tables(old_len, new_len, table, free_list, block_size: int, offset
     _run(dev, load_library().mca_block_tables, old_len.data_ptr(), new_len.data_ptr(), n, block_size, table.data_ptr(),
          table.stride(0) if n > 1 else width, width, free_list.data_ptr(), free_list.numel(),
          offsets.data_ptr(), slots.data_ptr(), slots.numel(), status.data_ptr())
+    increment_version((table, free_list, offsets, slots, status))
 
 
 def mca_cache_append(k, v, k_cache, v_cache, slots, rows=None):
     """Row i (rows[i] with rows) of k and v [n_src, n_kv_head, head_dim] into slot slots[i] of the caches
     [n_blocks, n_kv_head, block_size, head_dim]."""
+    if is_grad_enabled() and (k.requires_grad or v.requires_grad or k_cache.requires_grad or v_cache.requires_grad):
+        _no_graph(k=k, v=v, k_cache=k_cache, v_cache=v_cache)
     dev, dt = _gpu(k_cache), k_cache.dtype
     a = mca_cache_append_args()
     a.dtype = _type(k_cache)
@@ -145,6 +156,7 @@ def mca_cache_append(k, v, k_cache, v_cache, slots, rows=None):
     a.k, a.v, a.k_cache, a.v_cache = k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr()
     a.slots = slots.data_ptr()
     _run(dev, load_library().mca_cache_append, ctypes.byref(a))
+    increment_version((k_cache, v_cache))
 
 
 # ---------------------------------------------------------------------------
@@ -216,6 +228,10 @@ def mca_tree_attention(q, k, v, k_cache, v_cache, table, lengths, offsets, paren
     1 / sqrt(head_dim).  Rows of a given out and lse behind the last request stay as they were; those of new ones
     are zero.
     """
+    if is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or k_cache.requires_grad or
+                              v_cache.requires_grad or (out is not None and out.requires_grad) or
+                              (lse is not None and lse.requires_grad)):
+        _no_graph(q=q, k=k, v=v, k_cache=k_cache, v_cache=v_cache, out=out, lse=lse)
     if out is None:
         out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
     if lse is None:
@@ -228,6 +244,7 @@ def mca_tree_attention(q, k, v, k_cache, v_cache, table, lengths, offsets, paren
         room = _room(dev, nbytes, workspace)
         a.workspace, a.workspace_bytes = room.data_ptr(), room.numel()
     _run(dev, lib.mca_tree_attention, ctypes.byref(a))
+    increment_version((out, lse))
     return out, lse
 
 
@@ -265,7 +282,12 @@ def mca_token_logprobs_plan(logits, n_top: int = 0) -> int:
 
 
 def mca_token_logprobs(logits, tokens, n_top: int = 0, workspace=None) -> TokenLogprobs:
-    """Log probabilities of tokens [n_rows] under logits [n_rows, n_vocab], entropies and the n_top alternatives."""
+    """Log probabilities of tokens [n_rows] under logits [n_rows, n_vocab], entropies and the n_top alternatives.
+
+    Their gradient is mca_token_logprobs_grad.
+    """
+    if logits.requires_grad and is_grad_enabled():
+        _no_graph(logits=logits)
     dev, row = _logits(logits, tokens)
     a = mca_token_logprobs_args()
     a.dtype, a.n_top, a.token_bytes = _type(logits), n_top, tokens.element_size()
@@ -288,6 +310,12 @@ def mca_token_logprobs(logits, tokens, n_top: int = 0, workspace=None) -> TokenL
 
 def mca_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, grad_entropy=None, out=None):
     """Gradient with respect to the logits of sum grad_logprob * logprob + grad_entropy * entropy; out may be logits."""
+    if is_grad_enabled() and (logits.requires_grad or lse.requires_grad or
+                              (entropy is not None and entropy.requires_grad) or
+                              (grad_logprob is not None and grad_logprob.requires_grad) or
+                              (grad_entropy is not None and grad_entropy.requires_grad) or
+                              (out is not None and out.requires_grad)):
+        _no_graph(logits=logits, lse=lse, entropy=entropy, grad_logprob=grad_logprob, grad_entropy=grad_entropy, out=out)
     dev, row = _logits(logits, tokens)
     n, f32 = logits.shape[0], torch.float32
     if out is None:
@@ -308,6 +336,7 @@ def mca_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, gra
         _flat(dev, f32, "entropy", entropy, n)
         a.grad_entropy, a.entropy = grad_entropy.data_ptr(), entropy.data_ptr()
     _run(dev, load_library().mca_token_logprobs_grad, ctypes.byref(a))
+    increment_version((out,))
     return out
 
 
@@ -352,6 +381,8 @@ def mca_extend(ctx: "mca.TransformerContext", tokens, parents, offsets, lengths,
     The work goes on the context's stream.  Where that is not the current one, the caller orders the two (inputs
     before the call, results after it); the memory of the tensors stays theirs until both streams are done with it.
     """
+    if is_grad_enabled() and any(t is not None and t.requires_grad for t in (k_cache, v_cache, qkv, logits)):
+        _no_graph(k_cache=k_cache, v_cache=v_cache, qkv=qkv, logits=logits)
     # the context's own device: its name may lack the index
     dev, desc = ctx.workspace.device, ctx.desc
     given = dict(tokens=tokens, parents=parents, offsets=offsets, lengths=lengths, table=table, k_cache=k_cache,
@@ -373,6 +404,7 @@ def mca_extend(ctx: "mca.TransformerContext", tokens, parents, offsets, lengths,
         room = _room(dev, nbytes.value, workspace)
         a.workspace, a.workspace_bytes = room.data_ptr(), room.numel()
         _check(lib.mca_extend(ctx.ctx, ctypes.byref(a)), ctx.ctx)
+    increment_version((qkv, logits))
     if caller != ctx.stream:
         for t in given.values():
             if t is not None:

@@ -23,3 +23,24 @@ def test_extend_refuses_tensors_of_another_device_than_the_contexts():
     ctx, args, outs = extend_args()
     with pytest.raises(mca.MCAError, match="is on cpu, not cuda:0"):
         lm.mca_extend(ctx, *args, **outs)
+
+
+def test_tensors_that_require_a_gradient_are_refused_while_gradients_are_recorded():
+    """Under no_grad they are taken (and refused here for another reason: there is no GPU)."""
+    z, t = torch.zeros(2, 5), torch.zeros(2, dtype=torch.int32)
+    g = torch.zeros(2, 5, requires_grad=True)
+    row, q, cache = torch.zeros(2), torch.zeros(2, 1, 8), torch.zeros(2, 1, 4, 8)
+    gq, gcache = q.clone().requires_grad_(), cache.clone().requires_grad_()
+    tail = (t[:, None], t, torch.zeros(3, dtype=torch.int32), t, 1)
+    ctx, args, outs = extend_args()
+    calls = [lambda: lm.mca_token_logprobs(g, t), lambda: lm.mca_token_logprobs(g * 2, t),
+             lambda: lm.mca_token_logprobs_grad(g, t, row, row, row), lambda: lm.mca_token_logprobs_grad(z, t, row, row, row, out=g),
+             lambda: lm.mca_cache_append(gq, q, cache, cache, t.long()), lambda: lm.mca_cache_append(q, q, cache, gcache, t.long()),
+             lambda: lm.mca_tree_attention(q, gq, q, cache, cache, *tail), lambda: lm.mca_tree_attention(q, q, q, gcache, cache, *tail),
+             lambda: lm.mca_tree_attention(q, q, q, cache, cache, *tail, out=gq),
+             lambda: lm.mca_extend(ctx, *args, **dict(outs, logits=outs["logits"].clone().requires_grad_()))]
+    for call in calls:
+        with pytest.raises(mca.MCAError, match="requires grad"):
+            call()
+        with torch.no_grad(), pytest.raises(mca.MCAError, match="cpu"):
+            call()

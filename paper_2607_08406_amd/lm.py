@@ -76,6 +76,13 @@ def _whole(device, dtype, what, t, shape):
         _refuse(f"{what} is not a contiguous tensor of shape {tuple(shape)}")
 
 
+def _int32(**numbers):
+    """The numbers go to the library in 32 bits, which ctypes would cut them to."""
+    for what, x in numbers.items():
+        if not 0 <= x < 1 << 31:
+            _refuse(f"{what} is {x}: out of range [0, 2^31)")
+
+
 def _no_graph(**tensors):
     what = next(what for what, t in tensors.items() if t is not None and t.requires_grad)
     _refuse(f"{what} requires grad, but the call records no graph: detach it, or call under torch.no_grad()")
@@ -113,6 +120,7 @@ def _room(device, nbytes, workspace):
 def mca_block_tables(old_len, new_len, table, free_list, block_size: int, offsets, slots, status):
     """Update table [n_req, max_blocks] and free_list [n_blocks] for requests that go from old_len to
     new_len [n_req] tokens; offsets [n_req + 1], slots [max_tokens] (int64) and status [4] are written."""
+    _int32(block_size=block_size)
     dev, i32 = _gpu(table), torch.int32
     _check_all(dev, i32, 2, table=table)
     n, width = table.shape
@@ -191,7 +199,11 @@ def _attention_args(q, k, v, k_cache, v_cache, table, lengths, offsets, parents,
     a.n_rows, a.n_head, a.head_dim = n, n_head, dim
     a.n_blocks, a.n_kv_head, a.block_size = n_blocks, n_kv_head, block_size
     a.n_req, a.max_blocks, a.max_nodes = n_req, max_blocks, max_nodes
-    a.max_len = max_blocks * block_size if max_len is None else max_len
+    if max_len is None:
+        max_len = max_blocks * block_size
+    if (max_nodes | max_len) >> 31:
+        _int32(max_nodes=max_nodes, max_len=max_len)
+    a.max_len = max_len
     a.scale = dim ** -0.5 if scale is None else scale
     a.table_stride = stride if n_req > 1 else max_blocks
     a.q, a.k, a.v, a.out = q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr()
@@ -207,8 +219,10 @@ def mca_tree_attention_plan(q, k_cache, n_req: int, max_blocks: int, max_nodes: 
     a.dtype = _type(q)
     a.n_rows, a.n_head, a.head_dim = q.shape
     a.n_blocks, a.n_kv_head, a.block_size, _ = k_cache.shape
-    a.n_req, a.max_blocks, a.max_nodes = n_req, max_blocks, max_nodes
-    a.max_len = max_blocks * a.block_size if max_len is None else max_len
+    if max_len is None:
+        max_len = max_blocks * a.block_size
+    _int32(n_req=n_req, max_blocks=max_blocks, max_nodes=max_nodes, max_len=max_len)
+    a.n_req, a.max_blocks, a.max_nodes, a.max_len = n_req, max_blocks, max_nodes, max_len
     return _plan(a, load_library().mca_tree_attention_plan)
 
 
@@ -275,6 +289,7 @@ def _logits(logits, tokens):
 
 def mca_token_logprobs_plan(logits, n_top: int = 0) -> int:
     """Workspace bytes of mca_token_logprobs on logits of this shape."""
+    _int32(n_top=n_top)
     a = mca_token_logprobs_args()
     a.dtype, a.n_top = _type(logits), n_top
     a.n_rows, a.n_vocab = logits.shape
@@ -289,6 +304,8 @@ def mca_token_logprobs(logits, tokens, n_top: int = 0, workspace=None) -> TokenL
     if logits.requires_grad and is_grad_enabled():
         _no_graph(logits=logits)
     dev, row = _logits(logits, tokens)
+    if n_top >> 31:
+        _int32(n_top=n_top)
     a = mca_token_logprobs_args()
     a.dtype, a.n_top, a.token_bytes = _type(logits), n_top, tokens.element_size()
     n, a.n_vocab = logits.shape
@@ -361,9 +378,12 @@ def _extend_args(dev, desc, tokens, parents, offsets, lengths, table, k_cache, v
     _whole(dev, f32, "v_cache", v_cache, k_cache.shape)
     _whole(dev, f32, "qkv", qkv, (desc.n_block, n, 3, H, 32))
     logits_row = _rows(dev, f32, "logits", logits, (n, desc.vocab))[0]
-    a.n_req, a.n_rows, a.max_nodes = R, n, max_nodes
+    a.n_req, a.n_rows = R, n
     a.n_blocks, a.block_size, a.max_blocks = k_cache.shape[1], k_cache.shape[3], table.shape[1]
-    a.max_len = a.max_blocks * a.block_size if max_len is None else max_len
+    if max_len is None:
+        max_len = a.max_blocks * a.block_size
+    _int32(max_nodes=max_nodes, max_len=max_len)
+    a.max_nodes, a.max_len = max_nodes, max_len
     a.table_stride = table.stride(0) if R > 1 else a.max_blocks
     a.cache_layer = k_cache.stride(0) if desc.n_block > 1 else 0
     a.logits_row = logits_row if n > 1 else desc.vocab

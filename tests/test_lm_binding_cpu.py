@@ -44,3 +44,20 @@ def test_tensors_that_require_a_gradient_are_refused_while_gradients_are_recorde
             call()
         with torch.no_grad(), pytest.raises(mca.MCAError, match="cpu"):
             call()
+
+
+@pytest.mark.parametrize("kw", [dict(max_len=2 ** 32), dict(max_len=2 ** 32 + 5), dict(max_nodes=2 ** 32 + 1), dict(n_req=2 ** 32 + 1),
+                                dict(max_blocks=2 ** 32 + 1), dict(max_blocks=2 ** 28), dict(max_len=-1), dict(max_nodes=-2 ** 32 + 1)])
+def test_numbers_beyond_32_bits_are_refused(kw):
+    """Not cut to what is left of them."""
+    q, cache = torch.empty(4, 2, 64), torch.empty(9, 1, 16, 64)
+    a = dict(n_req=2, max_blocks=4, max_nodes=2)
+    assert lm.mca_tree_attention_plan(q, cache, **a) == 0
+    with pytest.raises(mca.MCAError):
+        lm.mca_tree_attention_plan(q, cache, **{**a, **kw})
+
+
+def test_numbers_of_alternatives_beyond_32_bits_are_refused():
+    for n in (2 ** 32 + 3, -2 ** 32 + 3):
+        with pytest.raises(mca.MCAError):
+            lm.mca_token_logprobs_plan(torch.empty(2, 500), n)

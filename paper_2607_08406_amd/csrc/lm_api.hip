@@ -99,7 +99,7 @@ int mca_cache_append(const mca_cache_append_args* args, void* hip_stream) {
   if ((int64_t)a.n_kv_head * a.head_dim > (1 << 24)) return unsupported("a row has at most 2^24 values");
   if (a.n > kMaxGrid || a.n_src > kMaxInt) return unsupported("at most 2^24 - 1 rows");
   if (!strides_ok({a.k_row, a.k_head, a.v_row, a.v_head}, kMaxStride)) return invalid("strides must not be negative");
-  if (a.n == 0) return MCA_OK;
+  if (a.n == 0 || a.n_src == 0) return MCA_OK;  // every source row is outside an empty source
   if (!a.k || !a.v || !a.k_cache || !a.v_cache || !a.slots) return invalid("an array is NULL");
   if (!aligned(a.k, el) || !aligned(a.v, el) || !aligned(a.k_cache, el) || !aligned(a.v_cache, el) || !aligned(a.slots, 8) ||
       !aligned(a.rows, 4))

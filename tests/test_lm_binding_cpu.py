@@ -1,4 +1,5 @@
-"""What the binding of the language-model operators refuses before it calls the library."""
+"""What the binding of the language-model operators refuses before it calls the library, and calls of nothing."""
+import ctypes
 from types import SimpleNamespace
 
 import pytest
@@ -61,3 +62,12 @@ def test_numbers_of_alternatives_beyond_32_bits_are_refused():
     for n in (2 ** 32 + 3, -2 ** 32 + 3):
         with pytest.raises(mca.MCAError):
             lm.mca_token_logprobs_plan(torch.empty(2, 500), n)
+
+
+def test_rows_of_an_empty_source_are_skipped():
+    """There is no source row to take: nothing is enqueued, and the arrays may be NULL, as an empty tensor's is."""
+    a = mca.mca_cache_append_args(dtype=0, n_kv_head=2, head_dim=32, block_size=16, n_blocks=8, n=5, n_src=0, k_row=64,
+                                  k_head=32, v_row=64, v_head=32, k_cache=1 << 20, v_cache=1 << 20, slots=1 << 20, rows=1 << 20)
+    assert mca.load_library().mca_cache_append(ctypes.byref(a), None) == mca.MCA_OK
+    a.n_src = 1
+    assert mca.load_library().mca_cache_append(ctypes.byref(a), None) == mca.MCA_EINVAL

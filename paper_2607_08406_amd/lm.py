@@ -326,7 +326,10 @@ def mca_token_logprobs(logits, tokens, n_top: int = 0, workspace=None) -> TokenL
 
 
 def mca_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, grad_entropy=None, out=None):
-    """Gradient with respect to the logits of sum grad_logprob * logprob + grad_entropy * entropy; out may be logits."""
+    """Gradient with respect to the logits of sum grad_logprob * logprob + grad_entropy * entropy; out may be logits.
+
+    entropy may be None without grad_entropy.
+    """
     if is_grad_enabled() and (logits.requires_grad or lse.requires_grad or
                               (entropy is not None and entropy.requires_grad) or
                               (grad_logprob is not None and grad_logprob.requires_grad) or
@@ -350,6 +353,8 @@ def mca_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, gra
         a.grad_logprob = grad_logprob.data_ptr()
     if grad_entropy is not None:
         _flat(dev, f32, "grad_entropy", grad_entropy, n)
+        if entropy is None:
+            _refuse("grad_entropy takes the entropy")
         _flat(dev, f32, "entropy", entropy, n)
         a.grad_entropy, a.entropy = grad_entropy.data_ptr(), entropy.data_ptr()
     _run(dev, load_library().mca_token_logprobs_grad, ctypes.byref(a))

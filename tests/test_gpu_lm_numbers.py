@@ -1,4 +1,4 @@
-"""Numbers beyond 32 bits that a program gives as "no limit" are refused, not cut."""
+"""Numbers beyond 32 bits that a program gives as "no limit" are refused, not cut; and what may be left out."""
 import pytest
 import torch
 
@@ -20,3 +20,14 @@ def test_calls_refuse_numbers_beyond_32_bits():
                 lambda: lm.mca_block_tables(put([0]), put([3]), put([[0]]), put([0]), 2 ** 32 + 16, put([0, 0]), slots, status)):
         with pytest.raises(MCAError, match="2.31"):
             bad()
+
+
+def test_the_entropy_may_be_left_out_without_its_gradient():
+    from paper_2607_08406_amd import lm
+    from paper_2607_08406_amd.mca import MCAError
+    z, tok = torch.randn(3, 50, device="cuda"), torch.tensor([1, 2, 3], device="cuda")
+    r = lm.mca_token_logprobs(z, tok)
+    g = torch.randn(3, device="cuda")
+    assert torch.equal(lm.mca_token_logprobs_grad(z, tok, r.lse, None, g), lm.mca_token_logprobs_grad(z, tok, r.lse, r.entropy, g))
+    with pytest.raises(MCAError, match="entropy"):
+        lm.mca_token_logprobs_grad(z, tok, r.lse, None, g, g)

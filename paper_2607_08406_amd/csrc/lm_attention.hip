@@ -35,13 +35,16 @@ constexpr float kLn2 = 0.6931471805599453f;
 // fp16 holds 2^-14 to 2^15 in full and steps of 2^-24 below, while the tokens that
 // make the result may all lie far below the largest weight (a first token that takes
 // nearly all weight and whose value is 0).  So the reference goes down as well: a
-// tile's largest weight is put at 2^11 and stays between 2^-8 and 2^15.  A weight then
+// tile's largest weight is put at 2^11, where a single one is exact (below that, by less
+// than a power, on the way down), and stays between 2^-8 and 2^15.  A weight then
 // is off by half a step of its own, or by 2^-25 where it is below 2^-14; over a tile
 // of 64 tokens the latter is 2^-11 of the tile's largest weight at the most, and
-// 2^-29 of it in a tile that has moved the reference.  The reference moves by whole
-// powers, which round nothing, and not below what leaves the sums under 2^80: tokens
-// that lie further down weigh less than 2^-69 of their row's together.  (The second
-// comparison costs 1 %: 16 drafts of 48, 192 to 384 rows, head_dim 128, 276 us against 273.)
+// 2^-29 of it in a tile that has moved the reference.  It moves down by whole powers,
+// which round nothing, and not below what leaves the sums under 2^80: tokens that lie
+// further down weigh less than 2^-69 of their row's together.  (The second
+// comparison costs 1 % at most, 4 % where scores are 4 times as large and references move
+// often: 16 drafts of 48, 192 to 384 rows, head_dim 128, 273 us with and without, 284
+// against 273.)
 template <int TYPE>
 struct Window {
   static constexpr bool kMoves = TYPE == MCA_TYPE_F16;
@@ -233,16 +236,18 @@ struct Rows {
       for (int t = 0; t < QT; ++t) {
         top[t] = fmaxf(top[t], __shfl_xor(top[t], 16, 64));
         top[t] = fmaxf(top[t], __shfl_xor(top[t], 32, 64));
-        float mn = fmaxf(m[t], top[t]);
+        float mn = fmaxf(m[t], top[t]), by = m[t] - mn;
         if constexpr (W::kMoves) {
-          const float put = ceilf(top[t]) - W::kPut;
           float sum = l[t] + __shfl_xor(l[t], 16, 64);
           sum += __shfl_xor(sum, 32, 64);
+          const float put = top[t] - W::kPut, whole = floorf(m[t] - put);
           // (not so if nothing is seen or a score is NaN)
-          const bool down = top[t] < m[t] - W::kBelow && sum * __builtin_amdgcn_exp2f(m[t] - put) <= W::kMost;
-          mn = down || top[t] > m[t] + W::kAbove ? put : m[t];
+          const bool down = top[t] < m[t] - W::kBelow && sum * __builtin_amdgcn_exp2f(whole) <= W::kMost;
+          const bool up = top[t] > m[t] + W::kAbove;
+          by = up ? m[t] - put : (down ? whole : 0.f);
+          mn = up ? put : m[t] - (down ? whole : 0.f);
         }
-        const float f = __builtin_amdgcn_exp2f(m[t] - mn);
+        const float f = __builtin_amdgcn_exp2f(by);
         m[t] = mn;
         l[t] *= f;
 #pragma unroll

@@ -123,3 +123,27 @@ def test_levels_too_far_apart_to_matter(lm):
     s, n = make("f16", scores, 2, 2, 64)
     for max_len in (1408, 1 << 17):
         check(lm, s, n, max_len)
+
+
+@pytest.mark.parametrize("typ", list(TYPES))
+@pytest.mark.parametrize("form", ["few", "chunks", "shared", "eight"])
+def test_a_single_token_is_exact(lm, typ, form):
+    """All weight lies on one token, whatever its score: nodes that see themselves alone, and cached tokens 40 above
+    the others.  The result is its value to the last bit (a weight of one power of two, and 2^-22 of its sum)."""
+    max_len, R, nodes, group = FORMS[form]
+    dim, dt, block = 64, TYPES[typ], 16
+    rng = np.random.default_rng(nodes)
+    n = min(max_len, 1200)
+    width = -(-n // block)
+    put = lambda a, t=torch.int32: torch.from_numpy(np.ascontiguousarray(a)).to(t).cuda()  # noqa: E731
+    T = 2 * nodes
+    q, k, v = rng.normal(size=(T, group, dim)), rng.normal(size=(T, 1, dim)), rng.normal(size=(T, 1, dim))
+    kc, vc = np.zeros((width, 1, block, dim)), rng.normal(size=(width, 1, block, dim))
+    at = n // 3
+    q[nodes:, :, 0], q[nodes:, :, 1:], k[nodes:, 0, 0] = 1.0, 0, -3.0
+    kc[at // block, 0, at % block, 0] = 40.28125
+    out, _ = lm.mca_tree_attention(put(q, dt), put(k, dt), put(v, dt), put(kc, dt), put(vc, dt),
+                                   put(np.tile(np.arange(width), (2, 1))), put([0, n]), put([0, nodes, T]), put(np.full(T, -1)),
+                                   nodes, max_len=max_len, scale=1.0)
+    assert torch.equal(out[:nodes], put(v, dt)[:nodes].expand(nodes, group, dim))
+    assert torch.equal(out[nodes:], put(vc, dt)[at // block, 0, at % block].expand(nodes, group, dim))

@@ -19,7 +19,8 @@
  *     device can see (lengths, offsets, block numbers, parents, tokens) is
  *     checked there and never leads to an access outside the arrays; each call
  *     says what such a value does.
- *   - Inputs and outputs must not overlap, except where a call says so.
+ *   - Inputs and outputs must not overlap, nor an output's rows each other,
+ *     except where a call says so.
  *   - Strides are in elements.  Vectors over the head dimension and over the
  *     vocabulary are contiguous.
  */

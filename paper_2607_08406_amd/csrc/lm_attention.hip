@@ -117,7 +117,7 @@ struct AttnDev {
 __device__ __forceinline__ int chunks_of(int len, int chunk) { return max(1, (len + chunk - 1) / chunk); }
 
 // The rows of a wave, 16 QT of them (node, head of the group), against tiles of
-// 32 NH tokens.  Everything stays in registers.  The products are transposed:
+// 32 NH tokens.  The products are transposed:
 // S^T = K Q^T gives lane (q, li) the scores of query li with tokens 4 q + v and
 // 16 + 4 q + v of the tile, which is already the operand layout of
 // O^T = V^T P^T if the product's index 8 q + j means token 4 q + j (j < 4) or
@@ -127,6 +127,12 @@ __device__ __forceinline__ int chunks_of(int len, int chunk) { return max(1, (le
 // dimension li * (dimensions of a lane) + e.  So no score and no value passes through
 // LDS to change its layout.  fp32 takes v_mfma_f32_16x16x4f32 with one token of a
 // lane a step.
+//
+// A tile is worked on in registers as far as they go.  By the compiler's remarks the
+// wide kernels of 16-bit values spill 13 to 17 (4 waves) or 31 to 35 (8) of 256 at
+// head_dim 65 to 128 with 32 rows a wave, 10 to 24 above 128, none below 65; and the
+// narrow fp32 kernel above 128 keeps whole arrays in 1152 bytes of scratch memory a lane
+// (100 requests of 2000, one row a head, 4 key heads: 2.1 TB/s at 256, 4.2 at 128).
 //
 // DP is head_dim rounded up; with PAD the missing dimensions are zero.
 template <int TYPE, int DP, int QT, int NH, bool PAD>
@@ -643,8 +649,8 @@ __global__ __launch_bounds__(kAttnThreads) void k_lm_attn(AttnDev p) {
 // cycles of a SIMD's matrix core over both products and about 8 vector instructions
 // (maximum, exponential, sum, packing) of a sixteenth of a cycle, which only another
 // wave's products hide.  16 requests of 4096 to 16384, 192 to 384 rows, 4 key heads of 128,
-// fp16 (95 GFLOP): 255 us and 26 of joining, 340 TFLOP/s of the 1217 that a large
-// product reaches; at 256 rows in each, 16384: 750.  One request of 262144, 96 rows,
+// fp16 (95 GFLOP): 258 us and 27 of joining, 340 TFLOP/s of the 1213 that a large
+// product reaches; of 16384, 512 rows, 8 key heads, bf16 830 and fp16 800.  One request of 262144, 96 rows,
 // 2 key heads of 64, bf16 (134 MB): 41 and 10.  16 rows of a wave, 32 requests of 8192
 // to 32768, one row a head, 8 key heads of 128, bf16 (2.63 GB): 465 and 8, 5.6 TB/s.
 template <int TYPE, int DP, int QT, int NW, bool PAD>
@@ -1086,6 +1092,13 @@ bool big_rows(const mca_tree_attention_args& a) { return a.head_dim > (a.dtype =
 // 504, but 128 of 8000 593 and 576).  Narrow fp32 rows are more work for the matrix
 // units than for memory, and a wide workgroup's waves without rows do none of it: 32
 // rows stay narrow (head_dim 64, 200 requests of 2000: 257 and 185; 64 rows 278 and 325).
+//
+// Where the rule takes the slower one (the one taken, and the other): it does not look
+// at head_dim, and above 128 a narrow workgroup's registers leave a CU one wave a SIMD
+// (256, 64 requests of 300, 24 rows 37 and 27, fp32 162 and 71, 48 rows 50 and 30; 8 of
+// 100000, 4 key heads, 4 rows 557 and 484, at 128 270 and 245); and many fp32 rows over
+// short contexts are too little for the wide kernel (16 of 1024, 256 rows, head_dim 64 91
+// and 65, 32 52 and 35; of 2048, 64 100 and 116).
 bool is_wide(const mca_tree_attention_args& a) {
   const int rows = shared_rows(a);
   const int64_t pairs = (int64_t)a.n_req * a.n_kv_head, reads = pairs * ((int64_t)a.max_len + a.max_nodes);

@@ -630,6 +630,9 @@ __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs_grad(mca_token_logpr
 
 // Short rows, and rows whose logits and gradient are not aligned alike: a
 // workgroup takes `rows` whole rows, value by value.  8192 rows of 65, fp32: 4.4 us.
+// Long rows pay for it: bf16, 4096 of 50257 values, the logits' 50304 apart and the
+// gradient's 50257, 537 us, and 142 with the gradient's 50304 apart too; 8 of 128000,
+// 128001 apart and 128000, 190 us and 4.5.
 template <int TYPE>
 __global__ __launch_bounds__(kLpThreads) void k_lm_logprobs_grad_flat(mca_token_logprobs_grad_args p, int rows) {
   typedef typename Elem<TYPE>::Raw Raw;

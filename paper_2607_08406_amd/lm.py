@@ -328,7 +328,8 @@ def mca_token_logprobs(logits, tokens, n_top: int = 0, workspace=None) -> TokenL
 def mca_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, grad_entropy=None, out=None):
     """Gradient with respect to the logits of sum grad_logprob * logprob + grad_entropy * entropy; out may be logits.
 
-    entropy may be None without grad_entropy.
+    entropy may be None without grad_entropy.  A new gradient is contiguous; logits whose rows lie further apart than
+    n_vocab are served several times faster with an out whose rows lie as far apart.
     """
     if is_grad_enabled() and (logits.requires_grad or lse.requires_grad or
                               (entropy is not None and entropy.requires_grad) or

@@ -1,0 +1,319 @@
+// HIP kernels (gfx950) of the paged cache of 8-bit values: rows quantised into
+// their places (mca_cache8_append) and read back (mca_cache8_read).
+//
+// A code is an e4m3 value, and a block's scale 2^e for one key head, so that a code
+// is one conversion from its value and back, a larger scale changes kept codes only
+// where they become subnormal, and neither the order nor the pieces in which a
+// block's tokens arrive change anything else.
+#include <algorithm>
+
+#include "device_common.hpp"
+#include "lm_device.hpp"
+#include "lm_kernels.hpp"
+
+namespace mca {
+
+namespace {
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kC8Threads = 256;
+constexpr int kC8Waves = kC8Threads / 64;
+constexpr int kC8Loads = 4;  // 16-byte loads of K and of V that a lane has in flight
+
+// Exponents of scales: the least (below it fp16 values would be no codes' values any
+// more; the others' stay normal numbers), and the one from which 256 times the scale
+// is past the type's largest value.
+template <int TYPE>
+struct Scale {
+  static constexpr int kLeast = TYPE == MCA_TYPE_F16 ? -15 : -100, kFull = TYPE == MCA_TYPE_F16 ? 8 : 120;
+};
+
+// The pages of all requests laid end to end with room to spare: request r's begin at
+// offsets[r] / B + 2 r, which leaves each at least its (tokens / B) + 2, and `items` of
+// the whole call can be had from what the host knows.  A wave looks 64 requests up
+// at a time.
+__device__ __forceinline__ int64_t first_item(const int32_t* offsets, int r, int B) {
+  return (int64_t)max(offsets[r], 0) / (unsigned)B + 2 * (int64_t)r;
+}
+__device__ __forceinline__ int request_of(const int32_t* offsets, int n_req, int B, int64_t item) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, hi = n_req;
+  while (true) {
+    const int step = (hi - lo + 63) / 64, at = lo + lane * step;
+    const int c = __popcll(__ballot(at < hi && first_item(offsets, at, B) <= item));
+    if (c == 0) return -1;
+    lo += (c - 1) * step;
+    hi = min(hi, lo + step);
+    if (step == 1) return lo;
+  }
+}
+
+// A request's page: its first row among the call's, positions and block.
+struct Page {
+  int64_t row0;  // of position `from`
+  int from, to;  // positions of the call's tokens in the page
+  int start, block;
+};
+template <class Args>
+__device__ __forceinline__ bool page_of(const Args& a, const int32_t* before, int64_t item, Page* p) {
+  const int r = request_of(a.offsets, a.n_req, a.block_size, item);
+  if (r < 0) return false;
+  const int64_t o0 = a.offsets[r], o1 = a.offsets[r + 1], len = before[r];
+  if (o0 < 0 || o1 <= o0 || o1 > a.n || len < 0) return false;
+  const int64_t page = len / a.block_size + (item - first_item(a.offsets, r, a.block_size));
+  const int64_t lo = max(len, page * a.block_size), hi = min(len + (o1 - o0), (page + 1) * a.block_size);
+  if (lo >= hi) return false;
+  p->row0 = o0 + (lo - len);
+  // positions behind max_blocks need not fit 32 bits
+  const bool in = page < a.max_blocks;
+  p->start = in ? (int)(page * a.block_size) : 0;
+  p->from = in ? (int)lo : 0;
+  p->to = p->from + (int)(hi - lo);
+  p->block = in ? a.table[(int64_t)r * a.table_stride + page] : -1;
+  if (p->block >= a.n_blocks) p->block = -1;
+  return true;
+}
+
+template <int TYPE>
+__device__ __forceinline__ void widen(u32x4 x, float (&f)[TYPE == MCA_TYPE_F32 ? 4 : 8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (TYPE == MCA_TYPE_F32) {
+      f[i] = __uint_as_float(x[i]);
+    } else if constexpr (TYPE == MCA_TYPE_BF16) {
+      f[2 * i] = __uint_as_float(x[i] << 16);
+      f[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
+    } else {
+      f[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)x[i]);
+      f[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(x[i] >> 16));
+    }
+  }
+}
+__device__ __forceinline__ bool finite_bits(uint32_t b) { return (b & 0x7f800000u) != 0x7f800000u; }
+// four codes, rounded to nearest, of values times 2^-e, none above `most`
+__device__ __forceinline__ uint32_t codes_of(const float* f, int e, float most) {
+  float y[4];
+  uint32_t nan = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool ok = finite_bits(__float_as_uint(f[i]));
+    y[i] = fminf(fmaxf(ok ? __builtin_ldexpf(f[i], -e) : 0.f, -most), most);
+    nan |= ok ? 0u : 0x7fu << (8 * i);
+  }
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+  return nan == 0 ? (uint32_t)w : ((uint32_t)w & ~(nan * 2 + (nan & 0x01010101u))) | nan;
+}
+// four kept codes in a scale 2^down times theirs (down <= 0); NaN stays as it is
+__device__ __forceinline__ uint32_t recoded(uint32_t codes, float by) {
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, by, false);
+  const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, by, true);
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(a[0], a[1], 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(b[0], b[1], w, true);
+  uint32_t nan = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (((codes >> (8 * i)) & 0x7f) == 0x7f) nan |= 0xffu << (8 * i);
+  return ((uint32_t)w & ~nan) | (codes & nan);
+}
+
+}  // namespace
+
+// W waves take one page of a request and one key head: largest values of K and V
+// first, from all their new rows, then codes.  What fits kC8Loads loads of a lane (64
+// rows of 128, 16-bit, of 4 waves) stays in registers between the two.
+template <int TYPE, int W>
+__global__ __launch_bounds__(kC8Threads) void k_lm_append8(mca_cache8_append_args a, int64_t units) {
+  constexpr int EL = TYPE == MCA_TYPE_F32 ? 4 : 2, VE = 16 / EL, T = 64 * W;
+  typedef Scale<TYPE> S;
+  __shared__ uint32_t s_top[2][kC8Waves];
+  const int wave = threadIdx.x >> 6, tid = threadIdx.x % T;
+  const int64_t unit = (int64_t)blockIdx.x * (kC8Waves / W) + wave / W;
+  Page pg{};
+  const bool any = unit < units && page_of(a, a.lengths, unit / a.n_kv_head, &pg) && pg.block >= 0;
+  if (!any) return;  // the same for all waves of a unit
+  const int h = (int)(unit % a.n_kv_head);
+  const int per = a.head_dim / VE, tokens = pg.to - pg.from, all = tokens * per;
+  const int64_t at = ((int64_t)pg.block * a.n_kv_head + h);
+  const int keep = max(0, pg.from - pg.start);
+  const uint32_t was_k = a.k_scale[at], was_v = a.v_scale[at];
+  u32x4 kx[kC8Loads], vx[kC8Loads];
+  auto load = [&](int c) {
+#pragma unroll
+    for (int u = 0; u < kC8Loads; ++u) {
+      const int e = c + tid + T * u;
+      kx[u] = vx[u] = u32x4{0, 0, 0, 0};
+      if (e < all) {
+        const int t = e / per, part = e - t * per;
+        const int64_t row = a.rows != nullptr ? (int64_t)a.rows[pg.row0 + t] : pg.row0 + t;
+        if (row >= 0 && row < a.n_src) {
+          kx[u] = gload((const u32x4*)((const char*)a.k + (row * a.k_row + h * a.k_head) * EL) + part);
+          vx[u] = gload((const u32x4*)((const char*)a.v + (row * a.v_row + h * a.v_head) * EL) + part);
+        }
+      }
+    }
+  };
+  uint32_t top_k = 0, top_v = 0;
+  auto look = [&](u32x4 x, uint32_t* top) {
+    float f[VE];
+    widen<TYPE>(x, f);
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+      const uint32_t b = __float_as_uint(f[i]) & 0x7fffffffu;
+      *top = max(*top, finite_bits(b) ? b : 0u);
+    }
+  };
+  const int last = (all - 1) / (T * kC8Loads) * (T * kC8Loads);
+  for (int c = 0; c <= last; c += T * kC8Loads) {
+    load(c);
+#pragma unroll
+    for (int u = 0; u < kC8Loads; ++u) {
+      look(kx[u], &top_k);
+      look(vx[u], &top_v);
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    top_k = max(top_k, (uint32_t)__shfl_xor(top_k, d, 64));
+    top_v = max(top_v, (uint32_t)__shfl_xor(top_v, d, 64));
+  }
+  if constexpr (W > 1) {
+    if ((threadIdx.x & 63) == 0) {
+      s_top[0][wave] = top_k;
+      s_top[1][wave] = top_v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      top_k = max(top_k, s_top[0][w]);
+      top_v = max(top_v, s_top[1][w]);
+    }
+  }
+  // 448 is 1.75 times 2^8
+  auto exponent = [&](uint32_t top, uint32_t was, int* before) {
+    const int e = max((int)(top >> 23) - 127 - 8 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0), S::kLeast);
+    *before = (int)min(max(was, 1u), 254u) - 127;
+    return keep > 0 ? max(e, *before) : e;
+  };
+  int old_k, old_v;
+  const int ek = exponent(top_k, was_k, &old_k), ev = exponent(top_v, was_v, &old_v);
+  if (tid == 0) {
+    a.k_scale[at] = (uint8_t)(ek + 127);
+    a.v_scale[at] = (uint8_t)(ev + 127);
+  }
+  uint8_t* kc = a.k_cache + at * a.block_size * a.head_dim;
+  uint8_t* vc = a.v_cache + at * a.block_size * a.head_dim;
+  const float most_k = ek >= S::kFull ? 240.f : 448.f, most_v = ev >= S::kFull ? 240.f : 448.f;
+  for (int c = last; c >= 0; c -= T * kC8Loads) {
+    if (c != last) load(c);
+#pragma unroll
+    for (int u = 0; u < kC8Loads; ++u) {
+      const int e = c + tid + T * u;
+      if (e >= all) continue;
+      const int64_t to = (int64_t)(pg.from - pg.start) * a.head_dim + (int64_t)e * VE;
+      float f[VE];
+      auto put = [&](u32x4 x, uint8_t* cache, int ex, float most) {
+        widen<TYPE>(x, f);
+        if constexpr (VE == 4)
+          gstore((uint32_t*)(cache + to), codes_of(f, ex, most));
+        else
+          gstore((u32x2*)(cache + to), u32x2{codes_of(f, ex, most), codes_of(f + 4, ex, most)});
+      };
+      put(kx[u], kc, ek, most_k);
+      put(vx[u], vc, ev, most_v);
+    }
+  }
+  if (keep > 0) {
+    auto again = [&](uint8_t* cache, int down) {
+      if (down >= 0) return;
+      const float by = __builtin_ldexpf(1.0f, max(down, -60));  // smaller: all codes 0 as well
+      for (int e = tid; e < keep * a.head_dim / 16; e += T) {
+        u32x4 x = gload((const u32x4*)cache + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = recoded(x[i], by);
+        gstore((u32x4*)cache + e, x);
+      }
+    };
+    again(kc, old_k - ek);
+    again(vc, old_v - ev);
+  }
+}
+
+// W waves take one page of a request and one key head: VE codes of K and of V a lane
+// and round, their values to the request's rows.
+template <int TYPE, int W>
+__global__ __launch_bounds__(kC8Threads) void k_lm_read8(mca_cache8_read_args a, int64_t units) {
+  constexpr int EL = TYPE == MCA_TYPE_F32 ? 4 : 2, VE = 16 / EL, CW = VE / 4, T = 64 * W;
+  const int wave = threadIdx.x >> 6, tid = threadIdx.x % T;
+  const int64_t unit = (int64_t)blockIdx.x * (kC8Waves / W) + wave / W;
+  Page pg{};
+  if (unit >= units || !page_of(a, a.start, unit / a.n_kv_head, &pg)) return;
+  const int h = (int)(unit % a.n_kv_head);
+  const int per = a.head_dim / VE, all = (pg.to - pg.from) * per;
+  const bool there = pg.block >= 0;
+  const int64_t at = (int64_t)max(pg.block, 0) * a.n_kv_head + h;
+  const float fk = scale_of(a.k_scale[at]), fv = scale_of(a.v_scale[at]);
+  const int64_t base = at * a.block_size * a.head_dim + (int64_t)(pg.from - pg.start) * a.head_dim;
+  for (int c = tid; c < all; c += T * kC8Loads) {
+    uint32_t kx[kC8Loads][CW], vx[kC8Loads][CW];
+#pragma unroll
+    for (int u = 0; u < kC8Loads; ++u) {
+      const int e = c + T * u;
+#pragma unroll
+      for (int i = 0; i < CW; ++i) kx[u][i] = vx[u][i] = 0;
+      if (there && e < all) {
+        load_codes<VE>((const char*)a.k_cache + base + (int64_t)e * VE, kx[u]);
+        load_codes<VE>((const char*)a.v_cache + base + (int64_t)e * VE, vx[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kC8Loads; ++u) {
+      const int e = c + T * u;
+      if (e >= all) continue;
+      const int t = e / per, part = e - t * per;
+      const int64_t row = pg.row0 + t;
+      gstore((u32x4*)((char*)a.k + (row * a.k_row + h * a.k_head) * EL) + part, wide_part<TYPE>(kx[u], fk));
+      gstore((u32x4*)((char*)a.v + (row * a.v_row + h * a.v_head) * EL) + part, wide_part<TYPE>(vx[u], fv));
+    }
+  }
+}
+
+namespace {
+
+// Waves of a page and head: one while a page's new rows are few.
+template <class Args>
+bool four_waves(const Args& a) {
+  const int64_t tokens = std::min<int64_t>(a.block_size, (a.n + a.n_req - 1) / a.n_req);
+  return tokens * a.head_dim >= 2048;
+}
+
+}  // namespace
+
+hipError_t lm_launch_append8(const mca_cache8_append_args& a, hipStream_t s) {
+  const int64_t units = (a.n / a.block_size + 2 * (int64_t)a.n_req) * a.n_kv_head;
+  const bool four = four_waves(a);
+  const dim3 grid((unsigned)(four ? units : (units + kC8Waves - 1) / kC8Waves)), threads(kC8Threads);
+  auto go = [&](auto one, auto more) { hipLaunchKernelGGL(four ? more : one, grid, threads, 0, s, a, units); };
+  switch (a.dtype) {
+    case MCA_TYPE_F32: go(k_lm_append8<MCA_TYPE_F32, 1>, k_lm_append8<MCA_TYPE_F32, kC8Waves>); break;
+    case MCA_TYPE_BF16: go(k_lm_append8<MCA_TYPE_BF16, 1>, k_lm_append8<MCA_TYPE_BF16, kC8Waves>); break;
+    default: go(k_lm_append8<MCA_TYPE_F16, 1>, k_lm_append8<MCA_TYPE_F16, kC8Waves>); break;
+  }
+  return hipGetLastError();
+}
+
+hipError_t lm_launch_read8(const mca_cache8_read_args& a, hipStream_t s) {
+  const int64_t units = (a.n / a.block_size + 2 * (int64_t)a.n_req) * a.n_kv_head;
+  const bool four = four_waves(a);
+  const dim3 grid((unsigned)(four ? units : (units + kC8Waves - 1) / kC8Waves)), threads(kC8Threads);
+  auto go = [&](auto one, auto more) { hipLaunchKernelGGL(four ? more : one, grid, threads, 0, s, a, units); };
+  switch (a.dtype) {
+    case MCA_TYPE_F32: go(k_lm_read8<MCA_TYPE_F32, 1>, k_lm_read8<MCA_TYPE_F32, kC8Waves>); break;
+    case MCA_TYPE_BF16: go(k_lm_read8<MCA_TYPE_BF16, 1>, k_lm_read8<MCA_TYPE_BF16, kC8Waves>); break;
+    default: go(k_lm_read8<MCA_TYPE_F16, 1>, k_lm_read8<MCA_TYPE_F16, kC8Waves>); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace mca

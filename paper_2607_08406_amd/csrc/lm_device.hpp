@@ -1,12 +1,16 @@
-// What the operators over requests read of a request.
+// What the operators over requests read of a request, and values of 8, 16 and 32 bits.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "device_common.hpp"
 #include "mca_lm.h"
 
 namespace mca {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // Cached tokens of request r that count.
 __device__ __forceinline__ int cached_of(const mca_tree_attention_args& a, int r) {
@@ -19,6 +23,84 @@ __device__ __forceinline__ bool rows_of(const mca_tree_attention_args& a, int r,
   *first = (int)f;
   *n = (int)(e - f);
   return f >= 0 && e > f && e <= a.n_rows && e - f <= a.max_nodes;
+}
+
+// Values of 8 bits (e4m3): the low or high two of a word, or all four, times a power of
+// two, exactly unless they pass the type's range.
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(min(max(byte, 1u), 254u) << 23); }
+template <int TYPE, bool HIGH>
+__device__ __forceinline__ uint32_t wide2(uint32_t codes, float scale) {
+  if constexpr (TYPE == MCA_TYPE_BF16)
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, HIGH));
+  else
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, HIGH));
+}
+template <bool HIGH>
+__device__ __forceinline__ u32x2 wide2_f32(uint32_t codes, float scale) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, scale, HIGH));
+}
+// 16 bytes of TYPE from 16 / EL codes
+template <int TYPE>
+__device__ __forceinline__ u32x4 wide_part(const uint32_t* codes, float scale) {
+  if constexpr (TYPE == MCA_TYPE_F32) {
+    const u32x2 a = wide2_f32<false>(codes[0], scale), b = wide2_f32<true>(codes[0], scale);
+    return u32x4{a[0], a[1], b[0], b[1]};
+  } else {
+    return u32x4{wide2<TYPE, false>(codes[0], scale), wide2<TYPE, true>(codes[0], scale), wide2<TYPE, false>(codes[1], scale),
+                 wide2<TYPE, true>(codes[1], scale)};
+  }
+}
+template <int BYTES>
+__device__ __forceinline__ void load_codes(const char* p, uint32_t* out) {
+  if constexpr (BYTES == 2) {
+    out[0] = gload((const uint16_t*)p);
+  } else if constexpr (BYTES == 4) {
+    out[0] = gload((const uint32_t*)p);
+  } else if constexpr (BYTES == 8) {
+    const u32x2 v = gload((const u32x2*)p);
+    out[0] = v[0];
+    out[1] = v[1];
+  } else {
+    const u32x4 v = gload((const u32x4*)p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = v[i];
+  }
+}
+
+// Values of a type.
+template <int TYPE>
+struct Elem {
+  static constexpr int kSize = 2, kPer = 8;  // bytes, values of 16 bytes
+  typedef uint16_t Raw;
+};
+template <>
+struct Elem<MCA_TYPE_F32> {
+  static constexpr int kSize = 4, kPer = 4;
+  typedef uint32_t Raw;
+};
+template <int TYPE>
+__device__ __forceinline__ float to_f32(typename Elem<TYPE>::Raw x) {
+  if constexpr (TYPE == MCA_TYPE_F32) return __uint_as_float(x);
+  if constexpr (TYPE == MCA_TYPE_BF16) return __uint_as_float((uint32_t)x << 16);
+  return (float)__builtin_bit_cast(_Float16, (uint16_t)x);
+}
+template <int TYPE>
+__device__ __forceinline__ typename Elem<TYPE>::Raw from_f32(float x) {
+  if constexpr (TYPE == MCA_TYPE_F32) return __float_as_uint(x);
+  if constexpr (TYPE == MCA_TYPE_BF16) return __builtin_bit_cast(uint16_t, (__bf16)x);
+  return __builtin_bit_cast(uint16_t, (_Float16)x);
+}
+template <int TYPE>
+__device__ __forceinline__ void unpack(u32x4 x, float (&f)[Elem<TYPE>::kPer]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (TYPE == MCA_TYPE_F32) {
+      f[i] = __uint_as_float(x[i]);
+    } else {
+      f[2 * i] = to_f32<TYPE>((uint16_t)(x[i] & 0xffff));
+      f[2 * i + 1] = to_f32<TYPE>((uint16_t)(x[i] >> 16));
+    }
+  }
 }
 
 }  // namespace mca

@@ -1,0 +1,495 @@
+// HIP kernels (gfx950) of distillation from a teacher's most probable symbols
+// (mca_distill) and its gradient (mca_distill_grad).
+//
+// The teacher's part of a row is at most 32 entries, worked on in 64 bits by one
+// wave; the student's is one pass over the logits for a sum of exponentials.  With
+// `rest` that is the sum over the symbols that are none of the teacher's, relative to
+// the largest of those, and the teacher's are added behind the pass: the loss takes the
+// logarithm of the first, which a difference of nearly equal sums, or exponentials relative
+// to the largest logit of all, would lose where the teacher's symbols have nearly all
+// weight.  Which of a row's 16-byte vectors hold a teacher's symbol is a bit each in
+// LDS, so that the entries are compared only with those vectors' values.
+#include <algorithm>
+
+#include "device_common.hpp"
+#include "lm_device.hpp"
+#include "lm_kernels.hpp"
+
+namespace mca {
+
+namespace {
+
+constexpr int kDsThreads = 256;
+constexpr int kDsWaves = kDsThreads / 64;
+constexpr int kDsUnroll = 4;
+constexpr int kDsSmall = 1024;     // largest vocabulary of the wave-per-row kernels
+constexpr int kDsSplits = 64;      // most parts of a row
+constexpr int64_t kDsPart = 8192;  // symbols of a part at least
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// The sum s of exp(scale (z - m)) over a part of a row, m the largest logit of it (with
+// `rest` of the symbols that are none of the teacher's).
+struct Sums {
+  float m, s;
+  __device__ __forceinline__ void move(float to, float k2) {
+    s *= __builtin_amdgcn_exp2f((m - to) * k2);
+    m = to;
+  }
+  __device__ __forceinline__ void join(float m2, float s2, float k2) {
+    move(fmaxf(m, m2), k2);
+    s += s2 * __builtin_amdgcn_exp2f((m2 - m) * k2);
+  }
+};
+
+// A wave's lane j: entry j of row t (-1: none).
+struct Entry {
+  int id;
+  float logprob;
+};
+template <class Args>
+__device__ __forceinline__ Entry entry_of(const Args& p, int64_t t, int lane) {
+  Entry e{-1, 0.f};
+  if (lane < p.n_top) {
+    const int id = p.ids[t * p.n_top + lane];
+    if (id >= 0 && id < p.n_vocab) e = {id, p.logprob[t * p.n_top + lane]};
+  }
+  return e;
+}
+__device__ __forceinline__ double wave_sum(double x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
+  return x;
+}
+// The teacher's probabilities of the wave's entries, and of all other symbols.
+struct Teacher {
+  double q, rest, total;
+  bool any;
+};
+template <class Args>
+__device__ __forceinline__ Teacher teacher_of(const Args& p, const Entry& e) {
+  Teacher r;
+  r.any = __ballot(e.id >= 0) != 0;
+  double t = e.id >= 0 ? (double)e.logprob * (double)p.scale : -__builtin_huge_val();
+  if (p.rest == 0) {
+    double top = t;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) top = fmax(top, __shfl_xor(top, d, 64));
+    const bool none = top == -__builtin_huge_val() && __ballot(t != t) == 0;
+    r.q = none ? 0.0 : exp(t - top);
+    const double sum = wave_sum(r.q);
+    r.q = none ? 0.0 : r.q / sum;
+    r.rest = 0;
+    r.total = wave_sum(r.q);
+  } else {
+    r.q = exp(t);
+    const double sum = wave_sum(r.q);
+    r.rest = r.any ? fmax(1.0 - sum, 0.0) : 0.0;
+    r.total = sum + r.rest;
+    if (!(sum < __builtin_huge_val())) r.q = r.total = __builtin_nan("");
+  }
+  return r;
+}
+
+// The loss of row t from its sums (one wave).
+template <int TYPE>
+__device__ __forceinline__ void finish(const mca_distill_args& p, int64_t t, const Entry& e, float m, double s) {
+  const int lane = threadIdx.x & 63;
+  const double k = p.scale, inf = __builtin_huge_val();
+  const typename Elem<TYPE>::Raw* row = (const typename Elem<TYPE>::Raw*)p.logits + t * p.logits_row;
+  const Teacher q = teacher_of(p, e);
+  const double z = e.id >= 0 ? (double)to_f32<TYPE>(row[e.id]) : -inf;
+  // the sum over all symbols, relative to the largest of all
+  double top = m, all = s;
+  if (p.rest != 0) {
+    bool first = e.id >= 0;  // a symbol counts once
+    for (int j = 0; j < p.n_top; ++j) {
+      const int id = __shfl(e.id, j, 64);
+      if (j < lane && id == e.id) first = false;
+    }
+    if (z > top) top = z;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) top = fmax(top, __shfl_xor(top, d, 64));
+    all = s * exp(k * ((double)m - top)) + wave_sum(first ? exp(k * (z - top)) : 0.0);
+  }
+  // logarithms beside k times the largest, which cancels from the loss
+  const double la = all == 0 ? -inf : log(all), ls = s == 0 ? -inf : log(s);
+  double part = 0;
+  if (q.q != q.q)
+    part = q.q;
+  else if (q.q > 0)
+    part = z == -inf ? inf : q.q * (log(q.q) - (k * (z - top) - la));
+  double loss = wave_sum(part);
+  if (q.rest > 0) loss += s == 0 ? inf : q.rest * (log(q.rest) - (k * ((double)m - top) + ls - la));
+  if (all != all) loss = all;
+  if (lane == 0) {
+    p.loss[t] = q.any ? (float)loss : 0.f;
+    p.lse[t] = (float)(all == 0 ? -inf : k * top + la);
+    if (p.rest != 0) p.lse_rest[t] = (float)(s == 0 ? -inf : k * (double)m + ls);
+  }
+}
+
+// Which of a part's vectors hold a symbol of the teacher's: bits in LDS.
+constexpr int kFlagWords = 1024;  // of up to 32768 vectors at a time
+
+}  // namespace
+
+// Rows of more than kDsSmall symbols: a workgroup per row, or per part of one (grid y),
+// in one pass.
+template <int TYPE>
+__global__ __launch_bounds__(kDsThreads) void k_lm_distill(mca_distill_args p, int splits, Sums* parts) {
+  constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
+  typedef typename Elem<TYPE>::Raw Raw;
+  __shared__ uint32_t s_flag[kFlagWords];
+  __shared__ int s_id[MCA_MAX_TOP];
+  __shared__ Sums s_sums[kDsWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t t = blockIdx.x;
+  const int split = blockIdx.y, V = (int)p.n_vocab, K = p.n_top;
+  const float k2 = p.scale * kLog2e;
+  const Raw* row = (const Raw*)p.logits + t * p.logits_row;
+  const int head = (int)(((16 - ((uintptr_t)row & 15)) & 15) / EL);
+  const int nvec = (V - head) / VE, tail = V - head - nvec * VE;
+  const u32x4* vec = (const u32x4*)(row + head);
+  const int per = (nvec + splits - 1) / splits, v0 = min(split * per, nvec), v1 = min(nvec, v0 + per);
+  const Entry e = entry_of(p, t, lane);  // every wave has them
+  const bool rest = p.rest != 0;
+  if (wave == 0 && lane < K) s_id[lane] = e.id;
+  Sums a = {kLowest, 0.f};
+  // the values of symbols first .. first + VE - 1; `known`: some may be the teacher's
+  auto take = [&](float (&f)[VE], int first, bool known) {
+    if (known)
+      for (int j = 0; j < K; ++j) {
+        const int at = s_id[j] - first;
+        if (s_id[j] < 0 || at < 0 || at >= VE) continue;
+#pragma unroll
+        for (int i = 0; i < VE; ++i) f[i] = i == at ? -__builtin_huge_valf() : f[i];
+      }
+    float cm = f[0];
+#pragma unroll
+    for (int i = 1; i < VE; ++i) cm = fmaxf(cm, f[i]);
+    if (cm > a.m) a.move(cm, k2);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < VE; ++i) sum += __builtin_amdgcn_exp2f((f[i] - a.m) * k2);
+    a.s += sum;
+  };
+  auto take_some = [&](int v, int n) {
+    float f[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) f[i] = i < n ? to_f32<TYPE>(row[v + i]) : -__builtin_huge_valf();
+    take(f, v, rest);
+  };
+  __syncthreads();
+  if (head > 0 && split == 0 && tid == 0) take_some(0, head);
+  for (int c0 = v0; c0 < v1; c0 += 32 * kFlagWords) {
+    const int c1 = min(v1, c0 + 32 * kFlagWords);
+    if (rest) {
+      __syncthreads();
+      for (int i = tid; i < (c1 - c0 + 31) / 32; i += kDsThreads) s_flag[i] = 0;
+      __syncthreads();
+      if (wave == 0 && e.id >= head) {
+        const int v = (e.id - head) / VE;
+        if (v >= c0 && v < c1) atomicOr(&s_flag[(v - c0) >> 5], 1u << ((v - c0) & 31));
+      }
+      __syncthreads();
+    }
+    for (int b = c0 + wave * 64 * kDsUnroll; b < c1; b += kDsWaves * 64 * kDsUnroll) {
+      u32x4 x[kDsUnroll];
+#pragma unroll
+      for (int u = 0; u < kDsUnroll; ++u) x[u] = gload(vec + min(b + 64 * u + lane, c1 - 1));
+#pragma unroll
+      for (int u = 0; u < kDsUnroll; ++u) {
+        const int v = b + 64 * u + lane;
+        if (v >= c1) continue;
+        const bool known = rest && ((s_flag[(v - c0) >> 5] >> ((v - c0) & 31)) & 1);
+        float f[VE];
+        unpack<TYPE>(x[u], f);
+        take(f, head + v * VE, known);
+      }
+    }
+  }
+  if (tail > 0 && split == splits - 1 && tid == kDsThreads - 1) take_some(V - tail, tail);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) a.join(__shfl_xor(a.m, d, 64), __shfl_xor(a.s, d, 64), k2);
+  if (lane == 0) s_sums[wave] = a;
+  __syncthreads();
+  if (wave != 0) return;
+  a = s_sums[0];
+#pragma unroll
+  for (int w = 1; w < kDsWaves; ++w) a.join(s_sums[w].m, s_sums[w].s, k2);
+  if (splits == 1)
+    finish<TYPE>(p, t, e, a.m, a.s);
+  else if (lane == 0)
+    parts[t * splits + split] = a;
+}
+
+template <int TYPE>
+__global__ __launch_bounds__(64) void k_lm_distill_join(mca_distill_args p, int splits, const Sums* parts) {
+  const int lane = threadIdx.x;
+  const int64_t t = blockIdx.x;
+  const Sums x = lane < splits ? parts[t * splits + lane] : Sums{kLowest, 0.f};
+  float m = x.m;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+  const double f = exp((double)p.scale * ((double)x.m - (double)m));
+  finish<TYPE>(p, t, entry_of(p, t, lane), m, wave_sum(f * x.s));
+}
+
+// Rows of at most 64 N symbols: a wave per row, the row in registers.
+template <int TYPE, int N>
+__global__ __launch_bounds__(kDsThreads) void k_lm_distill_small(mca_distill_args p) {
+  typedef typename Elem<TYPE>::Raw Raw;
+  const int lane = threadIdx.x & 63;
+  const int64_t t = (int64_t)blockIdx.x * kDsWaves + (threadIdx.x >> 6);
+  if (t >= p.n_rows) return;
+  const int V = (int)p.n_vocab;
+  const Raw* row = (const Raw*)p.logits + t * p.logits_row;
+  const float k2 = p.scale * kLog2e;
+  const Entry e = entry_of(p, t, lane);
+  float z[N], m = kLowest, s = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) z[i] = lane + 64 * i < V ? to_f32<TYPE>(row[lane + 64 * i]) : -__builtin_huge_valf();
+  if (p.rest != 0) {
+    uint32_t mine = 0;  // which of the lane's symbols are the teacher's
+    for (int j = 0; j < p.n_top; ++j) {
+      const int id = __builtin_amdgcn_readlane(e.id, j);
+      if (id >= 0 && (id & 63) == lane) mine |= 1u << (id >> 6);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) z[i] = (mine >> i) & 1 ? -__builtin_huge_valf() : z[i];
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) m = fmaxf(m, z[i]);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+#pragma unroll
+  for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((z[i] - m) * k2);
+  finish<TYPE>(p, t, e, m, wave_sum((double)s));
+}
+
+namespace {
+
+// A row's gradient: factors of exp(scale z - lse) for symbols of the teacher's and of
+// exp(scale z - lse_other) for others, both at most 1, and what is taken off the teacher's.
+struct RowGrad {
+  float lse, lse_other, known, other;
+  bool zero;
+};
+__device__ __forceinline__ RowGrad row_grad(const mca_distill_grad_args& p, int64_t t, const Teacher& q, double* off) {
+  RowGrad r;
+  const double g = (double)p.grad_loss[t] * (double)p.scale;
+  r.lse = r.lse_other = p.lse[t];
+  r.zero = !q.any || r.lse == -__builtin_huge_valf();
+  r.known = r.other = (float)(g * q.total);
+  if (p.rest != 0) {
+    const float lr = p.lse_rest[t];
+    const bool none = lr == -__builtin_huge_valf();  // then the others' exponentials are 0
+    r.lse_other = none ? 0.f : lr;
+    r.other = none ? 0.f : (float)(g * (q.total * exp((double)lr - (double)r.lse) - q.rest));
+  }
+  *off = g * q.q;
+  return r;
+}
+__device__ __forceinline__ float prob(float z, float scale, float lse) {
+  return __builtin_amdgcn_exp2f(fmaf(z, scale, -lse) * kLog2e);
+}
+
+}  // namespace
+
+// Long rows: a workgroup takes 256 x kDsUnroll vectors of one row.
+template <int TYPE>
+__global__ __launch_bounds__(kDsThreads) void k_lm_distill_grad(mca_distill_grad_args p) {
+  constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
+  typedef typename Elem<TYPE>::Raw Raw;
+  __shared__ uint32_t s_flag[kDsThreads * kDsUnroll / 32];
+  __shared__ int s_id[MCA_MAX_TOP];
+  __shared__ float s_off[MCA_MAX_TOP];
+  __shared__ RowGrad s_row;
+  const int tid = threadIdx.x, lane = tid & 63, V = (int)p.n_vocab, K = p.n_top;
+  const int64_t t = blockIdx.y;
+  const Raw* row = (const Raw*)p.logits + t * p.logits_row;
+  Raw* out = (Raw*)p.grad + t * p.grad_row;
+  const int head = (int)(((16 - ((uintptr_t)row & 15)) & 15) / EL);
+  const int nvec = (V - head) / VE, tail = V - head - nvec * VE;
+  const u32x4* vec = (const u32x4*)(row + head);
+  u32x4* vout = (u32x4*)(out + head);
+  const int c0 = blockIdx.x * kDsThreads * kDsUnroll, b = c0 + tid;
+  u32x4 x[kDsUnroll];
+#pragma unroll
+  for (int u = 0; u < kDsUnroll; ++u)
+    if (b + kDsThreads * u < nvec) x[u] = gload(vec + b + kDsThreads * u);
+  if (tid < kDsThreads * kDsUnroll / 32) s_flag[tid] = 0;
+  __syncthreads();
+  if (tid < 64) {
+    const Entry e = entry_of(p, t, lane);
+    double off;
+    const RowGrad r = row_grad(p, t, teacher_of(p, e), &off);
+    if (lane < K) {
+      s_id[lane] = e.id;
+      s_off[lane] = (float)off;
+    }
+    if (lane == 0) s_row = r;
+    if (e.id >= head) {
+      const int v = (e.id - head) / VE - c0;
+      if (v >= 0 && v < kDsThreads * kDsUnroll) atomicOr(&s_flag[v >> 5], 1u << (v & 31));
+    }
+  }
+  __syncthreads();
+  const RowGrad r = s_row;
+  auto grads = [&](float (&f)[VE], int first, bool known) {
+    float y[VE];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) y[i] = r.zero ? 0.f : prob(f[i], p.scale, r.lse_other) * r.other;
+    if (known && !r.zero) {
+      uint32_t mine = 0;
+      for (int j = 0; j < K; ++j) {
+        const int at = s_id[j] - first;
+        if (s_id[j] < 0 || at < 0 || at >= VE) continue;
+#pragma unroll
+        for (int i = 0; i < VE; ++i)
+          if (i == at) y[i] = ((mine >> i) & 1 ? y[i] : prob(f[i], p.scale, r.lse) * r.known) - s_off[j];
+        mine |= 1u << at;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VE; ++i) f[i] = y[i];
+  };
+#pragma unroll
+  for (int u = 0; u < kDsUnroll; ++u) {
+    const int v = b + kDsThreads * u;
+    if (v >= nvec) continue;
+    float f[VE];
+    unpack<TYPE>(x[u], f);
+    grads(f, head + v * VE, (s_flag[(v - c0) >> 5] >> ((v - c0) & 31)) & 1);
+    u32x4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (TYPE == MCA_TYPE_F32)
+        y[i] = __float_as_uint(f[i]);
+      else
+        y[i] = from_f32<TYPE>(f[2 * i]) | ((uint32_t)from_f32<TYPE>(f[2 * i + 1]) << 16);
+    }
+    gstore(vout + v, y);
+  }
+  if (blockIdx.x == 0 && tid < head + tail) {
+    const int v = tid < head ? tid : V - tail + (tid - head);
+    float f[VE];
+    f[0] = to_f32<TYPE>(row[v]);
+#pragma unroll
+    for (int i = 1; i < VE; ++i) f[i] = 0.f;
+    // (of the VE values from v on only the first counts)
+    grads(f, v, true);
+    out[v] = from_f32<TYPE>(f[0]);
+  }
+}
+
+// Short rows, and rows whose logits and gradient are not aligned alike: a wave per row,
+// value by value.
+template <int TYPE>
+__global__ __launch_bounds__(kDsThreads) void k_lm_distill_grad_rows(mca_distill_grad_args p) {
+  typedef typename Elem<TYPE>::Raw Raw;
+  const int lane = threadIdx.x & 63, V = (int)p.n_vocab;
+  const int64_t t = (int64_t)blockIdx.x * kDsWaves + (threadIdx.x >> 6);
+  if (t >= p.n_rows) return;
+  const Raw* row = (const Raw*)p.logits + t * p.logits_row;
+  Raw* out = (Raw*)p.grad + t * p.grad_row;
+  const Entry e = entry_of(p, t, lane);
+  double off64;
+  const RowGrad r = row_grad(p, t, teacher_of(p, e), &off64);
+  const float off = (float)off64;
+  for (int v0 = 0; v0 < V; v0 += 64) {
+    const int v = v0 + lane;
+    const float z = v < V ? to_f32<TYPE>(row[v]) : 0.f;
+    float y = prob(z, p.scale, r.lse_other) * r.other;
+    bool known = false;
+    // the entries among these 64 symbols
+    for (uint64_t some = __ballot(e.id >= v0 && e.id < v0 + 64); some != 0; some &= some - 1) {
+      const int j = __builtin_ctzll(some);
+      const int id = __shfl(e.id, j, 64);
+      const float o = __shfl(off, j, 64);
+      if (id != v) continue;
+      y = (known ? y : prob(z, p.scale, r.lse) * r.known) - o;
+      known = true;
+    }
+    if (v < V) out[v] = from_f32<TYPE>(r.zero ? 0.f : y);
+  }
+}
+
+LogprobsPlan lm_distill_plan(const mca_distill_args& a) {
+  LogprobsPlan p{1, 0};
+  if (a.n_vocab <= 2 * kDsPart || a.n_rows == 0) return p;
+  const int64_t want = (1024 + a.n_rows - 1) / a.n_rows, most = (a.n_vocab + kDsPart - 1) / kDsPart;
+  p.splits = (int32_t)std::clamp<int64_t>(std::min(want, most), 1, kDsSplits);
+  if (p.splits > 1) p.bytes = (size_t)a.n_rows * p.splits * sizeof(Sums);
+  return p;
+}
+
+namespace {
+
+template <int TYPE>
+void launch_distill(const mca_distill_args& a, const LogprobsPlan& plan, hipStream_t s) {
+  const dim3 threads(kDsThreads), grid((unsigned)((a.n_rows + kDsWaves - 1) / kDsWaves));
+  if (a.n_vocab <= 128)
+    hipLaunchKernelGGL((k_lm_distill_small<TYPE, 2>), grid, threads, 0, s, a);
+  else if (a.n_vocab <= 256)
+    hipLaunchKernelGGL((k_lm_distill_small<TYPE, 4>), grid, threads, 0, s, a);
+  else if (a.n_vocab <= 512)
+    hipLaunchKernelGGL((k_lm_distill_small<TYPE, 8>), grid, threads, 0, s, a);
+  else if (a.n_vocab <= kDsSmall)
+    hipLaunchKernelGGL((k_lm_distill_small<TYPE, 16>), grid, threads, 0, s, a);
+  else {
+    Sums* parts = (Sums*)a.workspace;
+    hipLaunchKernelGGL((k_lm_distill<TYPE>), dim3((unsigned)a.n_rows, (unsigned)plan.splits), threads, 0, s, a, plan.splits, parts);
+    if (plan.splits > 1)
+      hipLaunchKernelGGL((k_lm_distill_join<TYPE>), dim3((unsigned)a.n_rows), dim3(64), 0, s, a, plan.splits, parts);
+  }
+}
+
+template <int TYPE>
+void launch_distill_grad(const mca_distill_grad_args& a, hipStream_t s) {
+  const int el = Elem<TYPE>::kSize;
+  const bool alike = (((uintptr_t)a.logits - (uintptr_t)a.grad) & 15) == 0 &&
+                     (((a.logits_row - a.grad_row) * el) & 15) == 0;
+  if (a.n_vocab >= 512 && alike) {
+    const int64_t per = (int64_t)kDsThreads * kDsUnroll * Elem<TYPE>::kPer;
+    for (int64_t t0 = 0; t0 < a.n_rows; t0 += 65535) {  // grid y
+      mca_distill_grad_args b = a;
+      b.n_rows = std::min<int64_t>(65535, a.n_rows - t0);
+      b.logits = (const char*)a.logits + t0 * a.logits_row * el;
+      b.grad = (char*)a.grad + t0 * a.grad_row * el;
+      b.logprob += t0 * a.n_top;
+      b.ids += t0 * a.n_top;
+      b.lse += t0;
+      if (b.lse_rest != nullptr) b.lse_rest += t0;
+      b.grad_loss += t0;
+      hipLaunchKernelGGL((k_lm_distill_grad<TYPE>), dim3((unsigned)((a.n_vocab + per - 1) / per), (unsigned)b.n_rows),
+                         dim3(kDsThreads), 0, s, b);
+    }
+  } else {
+    hipLaunchKernelGGL((k_lm_distill_grad_rows<TYPE>), dim3((unsigned)((a.n_rows + kDsWaves - 1) / kDsWaves)), dim3(kDsThreads),
+                       0, s, a);
+  }
+}
+
+}  // namespace
+
+hipError_t lm_launch_distill(const mca_distill_args& a, const LogprobsPlan& plan, hipStream_t s) {
+  switch (a.dtype) {
+    case MCA_TYPE_F32: launch_distill<MCA_TYPE_F32>(a, plan, s); break;
+    case MCA_TYPE_BF16: launch_distill<MCA_TYPE_BF16>(a, plan, s); break;
+    default: launch_distill<MCA_TYPE_F16>(a, plan, s); break;
+  }
+  return hipGetLastError();
+}
+
+hipError_t lm_launch_distill_grad(const mca_distill_grad_args& a, hipStream_t s) {
+  switch (a.dtype) {
+    case MCA_TYPE_F32: launch_distill_grad<MCA_TYPE_F32>(a, s); break;
+    case MCA_TYPE_BF16: launch_distill_grad<MCA_TYPE_BF16>(a, s); break;
+    default: launch_distill_grad<MCA_TYPE_F16>(a, s); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace mca

@@ -13,13 +13,12 @@
 #include <algorithm>
 
 #include "device_common.hpp"
+#include "lm_device.hpp"
 #include "lm_kernels.hpp"
 
 namespace mca {
 
 namespace {
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kLpThreads = 256;
 constexpr int kLpWaves = kLpThreads / 64;
@@ -39,41 +38,6 @@ constexpr float kFar = -1e30f;   // below every exponent; times 0 it is 0
 constexpr float kHuge = 1e38f;   // logits of this size times log2 e stay finite
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-
-template <int TYPE>
-struct Elem {
-  static constexpr int kSize = 2, kPer = 8;  // bytes, values of 16 bytes
-  typedef uint16_t Raw;
-};
-template <>
-struct Elem<MCA_TYPE_F32> {
-  static constexpr int kSize = 4, kPer = 4;
-  typedef uint32_t Raw;
-};
-template <int TYPE>
-__device__ __forceinline__ float to_f32(typename Elem<TYPE>::Raw x) {
-  if constexpr (TYPE == MCA_TYPE_F32) return __uint_as_float(x);
-  if constexpr (TYPE == MCA_TYPE_BF16) return __uint_as_float((uint32_t)x << 16);
-  return (float)__builtin_bit_cast(_Float16, (uint16_t)x);
-}
-template <int TYPE>
-__device__ __forceinline__ typename Elem<TYPE>::Raw from_f32(float x) {
-  if constexpr (TYPE == MCA_TYPE_F32) return __float_as_uint(x);
-  if constexpr (TYPE == MCA_TYPE_BF16) return __builtin_bit_cast(uint16_t, (__bf16)x);
-  return __builtin_bit_cast(uint16_t, (_Float16)x);
-}
-template <int TYPE>
-__device__ __forceinline__ void unpack(u32x4 x, float (&f)[Elem<TYPE>::kPer]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (TYPE == MCA_TYPE_F32) {
-      f[i] = __uint_as_float(x[i]);
-    } else {
-      f[2 * i] = to_f32<TYPE>((uint16_t)(x[i] & 0xffff));
-      f[2 * i + 1] = to_f32<TYPE>((uint16_t)(x[i] >> 16));
-    }
-  }
-}
 
 // Order of floats as positive numbers (equal for the two zeros), and back.
 __device__ __forceinline__ uint32_t sort_key(float x) {

@@ -1119,6 +1119,12 @@ size_t mca_struct_size(int32_t which) {
     case 9: return sizeof(mca_token_logprobs_args);
     case 10: return sizeof(mca_token_logprobs_grad_args);
     case 11: return sizeof(mca_extend_args);
+    case 12: return sizeof(mca_cache8_append_args);
+    case 13: return sizeof(mca_cache8_read_args);
+    case 14: return sizeof(mca_tree_attention8_args);
+    case 15: return sizeof(mca_verify_drafts_args);
+    case 16: return sizeof(mca_distill_args);
+    case 17: return sizeof(mca_distill_grad_args);
     default: return 0;
   }
 }

@@ -18,8 +18,9 @@ from torch import is_grad_enabled
 from torch._C import _cuda_getCurrentRawStream as _raw_stream, _increment_version as increment_version
 
 from . import mca
-from .mca import (MCA_EDEVICE, MCA_EINVAL, MCAError, _check, load_library, mca_cache_append_args, mca_extend_args,
-                  mca_token_logprobs_args, mca_token_logprobs_grad_args, mca_tree_attention_args)
+from .mca import (MCA_EDEVICE, MCA_EINVAL, MCAError, _check, load_library, mca_cache8_append_args, mca_cache8_read_args,
+                  mca_cache_append_args, mca_distill_args, mca_distill_grad_args, mca_extend_args, mca_token_logprobs_args,
+                  mca_token_logprobs_grad_args, mca_tree_attention8_args, mca_tree_attention_args, mca_verify_drafts_args)
 
 MCA_TYPE_F32, MCA_TYPE_BF16, MCA_TYPE_F16 = 0, 1, 2
 MCA_MAX_NODES, MCA_MAX_TOP, MCA_MAX_REQ = 128, 32, 65535
@@ -167,13 +168,86 @@ def mca_cache_append(k, v, k_cache, v_cache, slots, rows=None):
     increment_version((k_cache, v_cache))
 
 
+_E4M3 = torch.float8_e4m3fn
+
+
+def _cache8(a, dev, k_cache, v_cache, k_scale, v_scale, table):
+    """The cache of codes, its scales and table; returns the caches' shape."""
+    if k_cache.dim() != 4 or table.dim() != 2:
+        _refuse("k_cache has 4 dimensions, table 2")
+    shape = k_cache.shape
+    _whole(dev, _E4M3, "k_cache", k_cache, shape)
+    _whole(dev, _E4M3, "v_cache", v_cache, shape)
+    _whole(dev, torch.uint8, "k_scale", k_scale, shape[:2])
+    _whole(dev, torch.uint8, "v_scale", v_scale, shape[:2])
+    a.n_blocks, a.n_kv_head, a.block_size, a.head_dim = shape
+    n_req, max_blocks = table.shape
+    stride = _rows(dev, torch.int32, "table", table, table.shape)[0]
+    a.n_req, a.max_blocks, a.table_stride = n_req, max_blocks, stride if n_req > 1 else max_blocks
+    a.k_cache, a.v_cache, a.k_scale, a.v_scale = k_cache.data_ptr(), v_cache.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
+    a.table = table.data_ptr()
+    return shape
+
+
+def mca_cache8_append(k, v, k_cache, v_cache, k_scale, v_scale, table, lengths, offsets, rows=None):
+    """Quantise rows of k and v [n_src, n_kv_head, head_dim] into the caches (float8_e4m3fn, [n_blocks, n_kv_head,
+    block_size, head_dim]) and their scales (uint8, [n_blocks, n_kv_head]).
+
+    Request r, which has lengths[r] tokens, takes rows offsets[r] .. offsets[r + 1] - 1 (with rows, row rows[i] of k
+    and v for each of these i) behind them.
+    """
+    if is_grad_enabled() and (k.requires_grad or v.requires_grad):
+        _no_graph(k=k, v=v)
+    dev, dt = _gpu(k_cache), k.dtype
+    a = mca_cache8_append_args()
+    a.dtype = _type(k)
+    shape = _cache8(a, dev, k_cache, v_cache, k_scale, v_scale, table)
+    n_src = k.shape[0] if k.dim() else 0
+    src = (n_src, shape[1], shape[3])
+    a.k_row, a.k_head, _ = _rows(dev, dt, "k", k, src)
+    a.v_row, a.v_head, _ = _rows(dev, dt, "v", v, src)
+    _flat(dev, torch.int32, "lengths", lengths, a.n_req)
+    _flat(dev, torch.int32, "offsets", offsets, a.n_req + 1)
+    a.n = a.n_src = n_src
+    if rows is not None:
+        a.n = rows.numel()
+        _flat(dev, torch.int32, "rows", rows, a.n)
+        a.rows = rows.data_ptr()
+    a.k, a.v, a.lengths, a.offsets = k.data_ptr(), v.data_ptr(), lengths.data_ptr(), offsets.data_ptr()
+    _run(dev, load_library().mca_cache8_append, ctypes.byref(a))
+    increment_version((k_cache, v_cache, k_scale, v_scale))
+
+
+def mca_cache8_read(k, v, k_cache, v_cache, k_scale, v_scale, table, start, offsets):
+    """The values of tokens start[r], start[r] + 1, ... of each request r into rows offsets[r] .. offsets[r + 1] - 1 of
+    k and v [n, n_kv_head, head_dim], which are returned; other rows stay as they were."""
+    if is_grad_enabled() and (k.requires_grad or v.requires_grad):
+        _no_graph(k=k, v=v)
+    dev, dt = _gpu(k_cache), k.dtype
+    a = mca_cache8_read_args()
+    a.dtype = _type(k)
+    shape = _cache8(a, dev, k_cache, v_cache, k_scale, v_scale, table)
+    a.n = k.shape[0] if k.dim() else 0
+    to = (a.n, shape[1], shape[3])
+    a.k_row, a.k_head, _ = _rows(dev, dt, "k", k, to)
+    a.v_row, a.v_head, _ = _rows(dev, dt, "v", v, to)
+    _flat(dev, torch.int32, "start", start, a.n_req)
+    _flat(dev, torch.int32, "offsets", offsets, a.n_req + 1)
+    a.k, a.v, a.start, a.offsets = k.data_ptr(), v.data_ptr(), start.data_ptr(), offsets.data_ptr()
+    _run(dev, load_library().mca_cache8_read, ctypes.byref(a))
+    increment_version((k, v))
+    return k, v
+
+
 # ---------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------
 
-def _attention_args(q, k, v, k_cache, v_cache, table, lengths, offsets, parents, max_nodes, max_len, scale, out, lse):
+def _attention_args(q, k, v, k_cache, v_cache, table, lengths, offsets, parents, max_nodes, max_len, scale, out, lse,
+                    cache_dt=None, a=None):
     dev, dt, i32 = _gpu(q), q.dtype, torch.int32
-    a = mca_tree_attention_args()
+    a = mca_tree_attention_args() if a is None else a
+    cache_dt = dt if cache_dt is None else cache_dt
     a.dtype = _type(q)
     if q.dim() != 3 or k_cache.dim() != 4 or table.dim() != 2:
         _refuse("q has 3 dimensions, k_cache 4, table 2")
@@ -186,8 +260,8 @@ def _attention_args(q, k, v, k_cache, v_cache, table, lengths, offsets, parents,
     a.k_row, a.k_head, _ = _rows(dev, dt, "k", k, (n, n_kv_head, dim))
     a.v_row, a.v_head, _ = _rows(dev, dt, "v", v, (n, n_kv_head, dim))
     a.out_row, a.out_head, _ = _rows(dev, dt, "out", out, shape)
-    _whole(dev, dt, "k_cache", k_cache, cache)
-    _whole(dev, dt, "v_cache", v_cache, cache)
+    _whole(dev, cache_dt, "k_cache", k_cache, cache)
+    _whole(dev, cache_dt, "v_cache", v_cache, cache)
     n_req, max_blocks = table.shape
     stride = _rows(dev, i32, "table", table, table.shape)[0]
     _flat(dev, i32, "lengths", lengths, n_req)
@@ -215,7 +289,11 @@ def _attention_args(q, k, v, k_cache, v_cache, table, lengths, offsets, parents,
 
 def mca_tree_attention_plan(q, k_cache, n_req: int, max_blocks: int, max_nodes: int, max_len: Optional[int] = None) -> int:
     """Workspace bytes of mca_tree_attention on tensors of these shapes."""
-    a = mca_tree_attention_args()
+    return _plan(_attention_sizes(mca_tree_attention_args(), q, k_cache, n_req, max_blocks, max_nodes, max_len),
+                 load_library().mca_tree_attention_plan)
+
+
+def _attention_sizes(a, q, k_cache, n_req, max_blocks, max_nodes, max_len):
     a.dtype = _type(q)
     a.n_rows, a.n_head, a.head_dim = q.shape
     a.n_blocks, a.n_kv_head, a.block_size, _ = k_cache.shape
@@ -223,7 +301,7 @@ def mca_tree_attention_plan(q, k_cache, n_req: int, max_blocks: int, max_nodes: 
         max_len = max_blocks * a.block_size
     _int32(n_req=n_req, max_blocks=max_blocks, max_nodes=max_nodes, max_len=max_len)
     a.n_req, a.max_blocks, a.max_nodes, a.max_len = n_req, max_blocks, max_nodes, max_len
-    return _plan(a, load_library().mca_tree_attention_plan)
+    return a
 
 
 def _plan(a, call) -> int:
@@ -260,6 +338,113 @@ def mca_tree_attention(q, k, v, k_cache, v_cache, table, lengths, offsets, paren
     _run(dev, lib.mca_tree_attention, ctypes.byref(a))
     increment_version((out, lse))
     return out, lse
+
+
+def mca_tree_attention8_plan(q, k_cache, n_req: int, max_blocks: int, max_nodes: int, max_len: Optional[int] = None) -> int:
+    """Workspace bytes of mca_tree_attention8 on tensors of these shapes."""
+    a = mca_tree_attention8_args()
+    _attention_sizes(a.of, q, k_cache, n_req, max_blocks, max_nodes, max_len)
+    return _plan(a, load_library().mca_tree_attention8_plan)
+
+
+def mca_tree_attention8(q, k, v, k_cache, v_cache, k_scale, v_scale, table, lengths, offsets, parents, max_nodes: int,
+                        max_len: Optional[int] = None, scale: Optional[float] = None, out=None, lse=None,
+                        workspace=None):
+    """mca_tree_attention over caches of codes (float8_e4m3fn) with their scales (uint8, [n_blocks, n_kv_head]), as
+    mca_cache8_append leaves them; returns (out, lse)."""
+    if is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or
+                              (out is not None and out.requires_grad) or (lse is not None and lse.requires_grad)):
+        _no_graph(q=q, k=k, v=v, out=out, lse=lse)
+    if out is None:
+        out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.zeros(q.shape[:2], dtype=torch.float32, device=q.device)
+    a = mca_tree_attention8_args()
+    dev, of = _attention_args(q, k, v, k_cache, v_cache, table, lengths, offsets, parents, max_nodes, max_len, scale,
+                              out, lse, _E4M3, a.of)
+    _whole(dev, torch.uint8, "k_scale", k_scale, k_cache.shape[:2])
+    _whole(dev, torch.uint8, "v_scale", v_scale, k_cache.shape[:2])
+    a.k_scale, a.v_scale = k_scale.data_ptr(), v_scale.data_ptr()
+    lib = load_library()
+    nbytes = _plan(a, lib.mca_tree_attention8_plan)
+    if nbytes:
+        room = _room(dev, nbytes, workspace)
+        of.workspace, of.workspace_bytes = room.data_ptr(), room.numel()
+    _run(dev, lib.mca_tree_attention8, ctypes.byref(a))
+    increment_version((out, lse))
+    return out, lse
+
+
+# ---------------------------------------------------------------------------
+# verification of drafts
+# ---------------------------------------------------------------------------
+
+class DraftsVerified(NamedTuple):
+    new_len: torch.Tensor  # [n_req] int32: lengths and the nodes accepted
+    rows: torch.Tensor     # [n_rows] int32: the accepted nodes' rows, -1 behind the last
+    token: torch.Tensor    # [n_req] int32: the token that follows, -1 for none
+
+
+def _verify_args(target, draft, n_req, max_nodes, scale, draft_scale, greedy):
+    a = mca_verify_drafts_args()
+    a.dtype = _type(target)
+    if target.dim() != 2:
+        _refuse("target has 2 dimensions")
+    if max_nodes >> 31 or n_req >> 31:
+        _int32(max_nodes=max_nodes, n_req=n_req)
+    a.n_rows, a.n_vocab = target.shape
+    a.n_req, a.max_nodes, a.greedy, a.scale, a.draft_scale = n_req, max_nodes, bool(greedy), scale, draft_scale
+    if draft is not None and not greedy:
+        a.draft = draft.data_ptr()
+    return a
+
+
+def mca_verify_drafts_plan(target, draft, n_req: int, max_nodes: int, greedy: bool = False) -> int:
+    """Workspace bytes of mca_verify_drafts on tensors of these shapes."""
+    return _plan(_verify_args(target, draft, n_req, max_nodes, 1.0, 1.0, greedy), load_library().mca_verify_drafts_plan)
+
+
+def mca_verify_drafts(target, draft, tokens, parents, offsets, lengths, max_nodes: int, accept=None, sample=None,
+                      scale: float = 1.0, draft_scale: float = 1.0, greedy: bool = False, workspace=None) -> DraftsVerified:
+    """Which drafted nodes are accepted under the logits target [n_rows, n_vocab], and the token that follows.
+
+    Row t of target (and of draft, the logits that a node's children were drawn from; None if they were given) is
+    about what follows node t.  Request r has rows offsets[r] .. offsets[r + 1] - 1, the first of them the token before
+    the draft.  accept [n_rows] and sample [n_req] are random numbers in [0, 1) (float32); greedy takes none.
+    """
+    if is_grad_enabled() and (target.requires_grad or (draft is not None and draft.requires_grad)):
+        _no_graph(target=target, draft=draft)
+    dev, i32, f32 = _gpu(target), torch.int32, torch.float32
+    a = _verify_args(target, draft, lengths.numel(), max_nodes, scale, draft_scale, greedy)
+    n, n_vocab = target.shape
+    n_req = a.n_req
+    row = _rows(dev, target.dtype, "target", target, target.shape)[0]
+    a.target_row = row if n > 1 else n_vocab
+    a.target = target.data_ptr()
+    if a.draft:
+        row = _rows(dev, target.dtype, "draft", draft, target.shape)[0]
+        a.draft_row = row if n > 1 else n_vocab
+    _flat(dev, i32, "tokens", tokens, n)
+    _flat(dev, i32, "parents", parents, n)
+    _flat(dev, i32, "offsets", offsets, n_req + 1)
+    _flat(dev, i32, "lengths", lengths, n_req)
+    a.tokens, a.parents, a.offsets, a.lengths = tokens.data_ptr(), parents.data_ptr(), offsets.data_ptr(), lengths.data_ptr()
+    if not greedy:
+        if accept is None or sample is None:
+            _refuse("accept and sample are needed unless greedy")
+        _flat(dev, f32, "accept", accept, n)
+        _flat(dev, f32, "sample", sample, n_req)
+        a.accept, a.sample = accept.data_ptr(), sample.data_ptr()
+    new_len, token = torch.empty((2, n_req), dtype=i32, device=dev).unbind()
+    rows = torch.empty(n, dtype=i32, device=dev)
+    a.new_len, a.token, a.rows = new_len.data_ptr(), token.data_ptr(), rows.data_ptr()
+    lib = load_library()
+    nbytes = _plan(a, lib.mca_verify_drafts_plan)
+    if nbytes:
+        room = _room(dev, nbytes, workspace)
+        a.workspace, a.workspace_bytes = room.data_ptr(), room.numel()
+    _run(dev, lib.mca_verify_drafts, ctypes.byref(a))
+    return DraftsVerified(new_len, rows, token)
 
 
 # ---------------------------------------------------------------------------
@@ -359,6 +544,95 @@ def mca_token_logprobs_grad(logits, tokens, lse, entropy, grad_logprob=None, gra
         _flat(dev, f32, "entropy", entropy, n)
         a.grad_entropy, a.entropy = grad_entropy.data_ptr(), entropy.data_ptr()
     _run(dev, load_library().mca_token_logprobs_grad, ctypes.byref(a))
+    increment_version((out,))
+    return out
+
+
+# ---------------------------------------------------------------------------
+# distillation
+# ---------------------------------------------------------------------------
+
+class Distilled(NamedTuple):
+    loss: torch.Tensor      # [n_rows]
+    lse: torch.Tensor       # [n_rows]
+    lse_rest: torch.Tensor  # [n_rows], with rest, else [0]
+
+
+def _teacher(a, dev, logits, logprob, ids, rest, scale):
+    if logits.dim() != 2 or logprob.dim() != 2:
+        _refuse("logits and logprob have 2 dimensions")
+    n, n_vocab = logits.shape
+    a.dtype, a.rest, a.scale = _type(logits), bool(rest), scale
+    a.n_rows, a.n_vocab, a.n_top = n, n_vocab, logprob.shape[1]
+    row = _rows(dev, logits.dtype, "logits", logits, logits.shape)[0]
+    a.logits_row = row if n > 1 else n_vocab
+    shape = (n, a.n_top)
+    _whole(dev, torch.float32, "logprob", logprob, shape)
+    _whole(dev, torch.int32, "ids", ids, shape)
+    a.logits, a.logprob, a.ids = logits.data_ptr(), logprob.data_ptr(), ids.data_ptr()
+
+
+def mca_distill_plan(logits, n_top: int, rest: bool = False) -> int:
+    """Workspace bytes of mca_distill on logits of this shape."""
+    _int32(n_top=n_top)
+    a = mca_distill_args()
+    a.dtype, a.n_top, a.rest, a.scale = _type(logits), n_top, bool(rest), 1.0
+    a.n_rows, a.n_vocab = logits.shape
+    return _plan(a, load_library().mca_distill_plan)
+
+
+def mca_distill(logits, logprob, ids, rest: bool = False, scale: float = 1.0, workspace=None) -> Distilled:
+    """Each row's divergence of the student's logits [n_rows, n_vocab] from its teacher: log probabilities logprob
+    [n_rows, n_top] of the symbols ids (int32; outside the vocabulary: none), as top_logprob and top_id of
+    mca_token_logprobs are.
+
+    Without rest the teacher is renormalised over its symbols, both sides at the temperature 1 / scale; with it, all
+    other symbols are one more outcome (scale 1).  The gradient is mca_distill_grad.
+    """
+    if is_grad_enabled() and (logits.requires_grad or logprob.requires_grad):
+        _no_graph(logits=logits, logprob=logprob)
+    dev, f32 = _gpu(logits), torch.float32
+    a = mca_distill_args()
+    _teacher(a, dev, logits, logprob, ids, rest, scale)
+    n = a.n_rows
+    loss, lse, lse_rest = torch.empty((3, n), dtype=f32, device=dev).unbind()
+    if not rest:
+        lse_rest = lse_rest[:0]
+    a.loss, a.lse = loss.data_ptr(), lse.data_ptr()
+    if rest:
+        a.lse_rest = lse_rest.data_ptr()
+    lib = load_library()
+    nbytes = _plan(a, lib.mca_distill_plan)
+    if nbytes:
+        room = _room(dev, nbytes, workspace)
+        a.workspace, a.workspace_bytes = room.data_ptr(), room.numel()
+    _run(dev, lib.mca_distill, ctypes.byref(a))
+    return Distilled(loss, lse, lse_rest)
+
+
+def mca_distill_grad(logits, logprob, ids, lse, lse_rest, grad_loss, rest: bool = False, scale: float = 1.0, out=None):
+    """Gradient with respect to the logits of sum grad_loss * loss; lse and lse_rest as mca_distill gave them (lse_rest
+    is not read without rest).  out may be logits; where its rows are not aligned as the logits' are, long rows are
+    served more slowly."""
+    if is_grad_enabled() and any(t is not None and t.requires_grad for t in (logits, logprob, lse, lse_rest, grad_loss, out)):
+        _no_graph(logits=logits, logprob=logprob, lse=lse, lse_rest=lse_rest, grad_loss=grad_loss, out=out)
+    dev, f32 = _gpu(logits), torch.float32
+    a = mca_distill_grad_args()
+    _teacher(a, dev, logits, logprob, ids, rest, scale)
+    n = a.n_rows
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    row = _rows(dev, logits.dtype, "out", out, logits.shape)[0]
+    a.grad_row, a.grad = row if n > 1 else out.shape[1], out.data_ptr()
+    _flat(dev, f32, "lse", lse, n)
+    _flat(dev, f32, "grad_loss", grad_loss, n)
+    a.lse, a.grad_loss = lse.data_ptr(), grad_loss.data_ptr()
+    if rest:
+        if lse_rest is None:
+            _refuse("rest takes the lse_rest")
+        _flat(dev, f32, "lse_rest", lse_rest, n)
+        a.lse_rest = lse_rest.data_ptr()
+    _run(dev, load_library().mca_distill_grad, ctypes.byref(a))
     increment_version((out,))
     return out
 

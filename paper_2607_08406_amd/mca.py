@@ -145,8 +145,52 @@ class mca_extend_args(ctypes.Structure):
                [("workspace_bytes", ctypes.c_size_t)]
 
 
+class mca_cache8_append_args(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("dtype", "n_req", "n_kv_head", "head_dim", "block_size", "n_blocks", "max_blocks",
+                                    "reserved")] + \
+               [(n, _I64) for n in ("n", "n_src", "table_stride")] + [("k", _P), ("v", _P)] + \
+               [(n, _I64) for n in ("k_row", "k_head", "v_row", "v_head")] + \
+               [(n, _P) for n in ("k_cache", "v_cache", "k_scale", "v_scale", "table", "lengths", "offsets", "rows")]
+
+
+class mca_cache8_read_args(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("dtype", "n_req", "n_kv_head", "head_dim", "block_size", "n_blocks", "max_blocks",
+                                    "reserved")] + \
+               [("n", _I64), ("table_stride", _I64), ("k", _P), ("v", _P)] + \
+               [(n, _I64) for n in ("k_row", "k_head", "v_row", "v_head")] + \
+               [(n, _P) for n in ("k_cache", "v_cache", "k_scale", "v_scale", "table", "start", "offsets")]
+
+
+class mca_tree_attention8_args(ctypes.Structure):
+    _fields_ = [("of", mca_tree_attention_args), ("k_scale", _P), ("v_scale", _P)]
+
+
+class mca_verify_drafts_args(ctypes.Structure):
+    _fields_ = [(n, _I32) for n in ("dtype", "n_req", "max_nodes", "greedy")] + \
+               [(n, _I64) for n in ("n_rows", "n_vocab", "target_row", "draft_row")] + \
+               [("scale", ctypes.c_double), ("draft_scale", ctypes.c_double)] + \
+               [(n, _P) for n in ("target", "draft", "tokens", "parents", "offsets", "lengths", "accept", "sample",
+                                  "new_len", "rows", "token", "workspace")] + \
+               [("workspace_bytes", ctypes.c_size_t)]
+
+
+class mca_distill_args(ctypes.Structure):
+    _fields_ = [("dtype", _I32), ("n_top", _I32), ("rest", _I32), ("scale", ctypes.c_float)] + \
+               [(n, _I64) for n in ("n_rows", "n_vocab", "logits_row")] + \
+               [(n, _P) for n in ("logits", "logprob", "ids", "loss", "lse", "lse_rest", "workspace")] + \
+               [("workspace_bytes", ctypes.c_size_t)]
+
+
+class mca_distill_grad_args(ctypes.Structure):
+    _fields_ = [("dtype", _I32), ("n_top", _I32), ("rest", _I32), ("scale", ctypes.c_float)] + \
+               [(n, _I64) for n in ("n_rows", "n_vocab", "logits_row", "grad_row")] + \
+               [(n, _P) for n in ("logits", "logprob", "ids", "lse", "lse_rest", "grad_loss", "grad")]
+
+
 STRUCTS = [mca_net_desc, mca_cand, mca_data, mca_stats, mca_trace, mca_timing, mca_channel, mca_cache_append_args,
-           mca_tree_attention_args, mca_token_logprobs_args, mca_token_logprobs_grad_args, mca_extend_args]
+           mca_tree_attention_args, mca_token_logprobs_args, mca_token_logprobs_grad_args, mca_extend_args,
+           mca_cache8_append_args, mca_cache8_read_args, mca_tree_attention8_args, mca_verify_drafts_args,
+           mca_distill_args, mca_distill_grad_args]
 
 _SIGNATURES = {
     "mca_abi_version": (ctypes.c_int, []),
@@ -180,6 +224,15 @@ _SIGNATURES = {
     "mca_token_logprobs_plan": (ctypes.c_int, [_P, _P]),
     "mca_token_logprobs": (ctypes.c_int, [_P, _P]),
     "mca_token_logprobs_grad": (ctypes.c_int, [_P, _P]),
+    "mca_cache8_append": (ctypes.c_int, [_P, _P]),
+    "mca_cache8_read": (ctypes.c_int, [_P, _P]),
+    "mca_tree_attention8_plan": (ctypes.c_int, [_P, _P]),
+    "mca_tree_attention8": (ctypes.c_int, [_P, _P]),
+    "mca_verify_drafts_plan": (ctypes.c_int, [_P, _P]),
+    "mca_verify_drafts": (ctypes.c_int, [_P, _P]),
+    "mca_distill_plan": (ctypes.c_int, [_P, _P]),
+    "mca_distill": (ctypes.c_int, [_P, _P]),
+    "mca_distill_grad": (ctypes.c_int, [_P, _P]),
     "mca_extend_plan": (ctypes.c_int, [_P, _P, _P]),
     "mca_extend": (ctypes.c_int, [_P, _P]),
     "mca_destroy": (None, [_P]),

@@ -1,0 +1,252 @@
+"""The cache of 8-bit values: every byte against the fp64 oracle.
+
+Nothing here is off by anything: scales are powers of two, codes the nearest e4m3
+values (ties to even), and read values exact.
+"""
+import numpy as np
+import pytest
+import torch
+
+from lm8_util import TYPES, cache, codes, host, pages, put
+from oracle import lm as olm
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lm():
+    from paper_2607_08406_amd import lm as m
+    assert torch.cuda.is_available()
+    return m
+
+
+def make(seed, typ, old, new, kv, dim, block, gather=False, spread=2, size=1.0):
+    """Requests that go from old to old + new tokens; k and v are parts of one projection's rows."""
+    rng = np.random.default_rng(seed)
+    old, new = np.array(old), np.array(new)
+    table, blocks = pages(rng, old + new, block)
+    first = np.concatenate([[0], np.cumsum(new)])
+    n = int(first[-1])
+    src = n + 5 if gather else n + 2
+    x = rng.normal(size=(src, 3, kv, dim)) * size * np.exp(rng.normal(size=(src, 1, kv, 1)))
+    x = torch.from_numpy(x).to(TYPES[typ]).cuda()
+    rows = rng.permutation(src)[:n] if gather else None
+    (kc, ks), (vc, vs) = cache(rng, blocks, kv, block, dim, spread)
+    return dict(k=x[:, 1], v=x[:, 2], k_cache=codes(kc), v_cache=codes(vc), k_scale=put(ks, np.uint8), v_scale=put(vs, np.uint8),
+                table=put(table), lengths=put(old), offsets=put(first), rows=None if rows is None else put(rows))
+
+
+def expected(s, typ):
+    h = {n: host(t) for n, t in s.items()}
+    return olm.cache8_append(h["k"], h["v"], h["k_cache"], h["v_cache"], h["k_scale"], h["v_scale"], h["table"], h["lengths"],
+                             h["offsets"], h["rows"], typ)
+
+
+def check(lm, s, typ):
+    want = expected(s, typ)
+    lm.mca_cache8_append(**s)
+    for name, w in zip(("k_cache", "v_cache", "k_scale", "v_scale"), want):
+        got = host(s[name])
+        bad = np.nonzero(got != w)
+        assert len(bad[0]) == 0, (name, [b[:5] for b in bad], got[bad][:5], w[bad][:5])
+    return want
+
+
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("kv,dim,block", [(4, 32, 16), (2, 128, 64), (1, 80, 20), (3, 256, 7), (8, 16, 1), (1, 112, 33)])
+@pytest.mark.parametrize("gather", [False, True])
+def test_append(lm, typ, kv, dim, block, gather):
+    """Requests that begin, go on inside a block, at its border, take nothing, fill many blocks."""
+    s = make(7, typ, [0, 5, block, 3 * block - 1, 2, 0, 40], [1, 3, 1, 2, 0, 5 * block + 3, block], kv, dim, block, gather)
+    check(lm, s, typ)
+
+
+@pytest.mark.parametrize("typ", TYPES)
+def test_append_of_many_requests(lm, typ):
+    rng = np.random.default_rng(3)
+    s = make(8, typ, rng.integers(0, 100, 700), rng.integers(0, 4, 700), 2, 64, 16, True)
+    check(lm, s, typ)
+
+
+def test_the_same_call_again_changes_nothing(lm):
+    s = make(9, "bf16", [0, 5, 37], [20, 30, 9], 2, 64, 16)
+    want = check(lm, s, "bf16")
+    lm.mca_cache8_append(**s)
+    for name, w in zip(("k_cache", "v_cache", "k_scale", "v_scale"), want):
+        assert (host(s[name]) == w).all()
+
+
+def test_pieces_and_order(lm):
+    """Tokens one at a time, growing in size: the scale is that of all at once, codes too unless a kept value has
+    passed through a subnormal code."""
+    n, kv, dim, block = 24, 2, 64, 16
+    x = torch.randn(n, kv, dim, device="cuda") * torch.exp2(torch.arange(n, device="cuda") / 6.0)[:, None, None]
+    whole = make(1, "f32", [0], [n], kv, dim, block)
+    whole.update(k=x, v=x)
+    apart = {k: t.clone() if t is not None else None for k, t in whole.items()}
+    lm.mca_cache8_append(**whole)
+    for i in range(n):
+        apart.update(k=x[i:i + 1], v=x[i:i + 1], lengths=put([i]), offsets=put([0, 1]))
+        check(lm, apart, "f32")
+    blocks = whole["table"][0].long()
+    assert torch.equal(whole["k_scale"][blocks], apart["k_scale"][blocks])
+    a, b = (olm.e4m3_value(host(c["k_cache"][blocks])) for c in (whole, apart))
+    normal = np.abs(a) >= 2.0 ** -5
+    used = np.arange(2 * block).reshape(2, 1, block, 1) < n
+    assert (a == b)[normal & used].all() and np.abs(np.where(used, a - b, 0)).max() <= 2.0 ** -9
+
+
+@pytest.mark.parametrize("typ", TYPES)
+def test_extreme_values(lm, typ):
+    """Zeros, the type's largest and smallest values, infinities and NaN, ties of codes."""
+    big = torch.finfo(TYPES[typ]).max
+    s = make(4, typ, [0, 3, 0, 0, 0, 5], [4, 4, 4, 4, 4, 3], 1, 32, 8)
+    k = s["k"].clone()
+    k[0:4] = 0
+    k[4:8] *= 1e-30 if typ != "f16" else 1e-7
+    k[8:12, 0, :4] = torch.tensor([big, -big, big / 2, 1.0], dtype=k.dtype)
+    k[12, 0, 3] = float("nan")
+    k[13, 0, 4] = float("inf")
+    k[14, 0, 5] = -float("inf")
+    k[16:20] = (torch.arange(128, device="cuda").view(4, 1, 32) * 0.125 + 8).to(k.dtype)
+    k[20:23] = float("nan")
+    s["k"], s["v"] = k, (k.float() * 0.5).to(k.dtype)
+    check(lm, s, typ)
+    want = k.double()
+    out = torch.zeros_like(k)
+    lm.mca_cache8_read(out, torch.zeros_like(k), s["k_cache"], s["v_cache"], s["k_scale"], s["v_scale"], s["table"], s["lengths"],
+                       s["offsets"])
+    fin = torch.isfinite(want)
+    assert torch.isfinite(out[:23][fin[:23]]).all() and torch.isnan(out[:23][~fin[:23]]).all()
+    # 2^-4 of a value, or half a step of its block's subnormal codes: 2^-10 / 224 of the largest
+    top = torch.where(fin, want.abs(), 0.0).amax((1, 2), keepdim=True)
+    for a, b in ((0, 4), (8, 12), (12, 16), (16, 20)):
+        lim = torch.maximum(want[a:b].abs() / 16, top[a:b].amax() * 2.0 ** -10 / 224 + torch.finfo(k.dtype).tiny)
+        d = (out[a:b].double() - want[a:b]).abs()
+        assert (d <= lim)[fin[a:b]].all()
+
+
+def test_growth_beyond_every_kept_code(lm):
+    """Kept values of 2^-60 beside new ones of 2^60: codes 0, their sign kept; NaN codes stay."""
+    s = make(5, "f32", [5], [2], 1, 32, 8)
+    s["k_scale"].fill_(27)
+    s["v_scale"].fill_(1)
+    blk = int(s["table"][0, 0])
+    c = host(s["k_cache"])
+    c[blk, 0, 1, 3:5] = (0x7f, 0xff)
+    s["k_cache"] = codes(c)
+    s["k"] = s["k"] * 2.0 ** 60
+    s["v"] = s["v"] * 2.0 ** 100
+    check(lm, s, "f32")
+
+
+def test_scale_bytes_at_their_ends(lm):
+    """0 and 255 count as 1 and 254, in an append behind them and when read."""
+    for byte in (0, 1, 254, 255):
+        s = make(6, "f32", [5], [2], 1, 32, 8)
+        s["k_scale"].fill_(byte)
+        s["v_scale"].fill_(byte)
+        got = [torch.zeros(5, 1, 32, device="cuda") for _ in range(2)]
+        args = (s["k_cache"], s["v_cache"], s["k_scale"], s["v_scale"], s["table"])
+        lm.mca_cache8_read(*got, *args, put([0]), put([0, 5]))
+        want = olm.cache8_read(olm.cache8_values(host(s["k_cache"]), host(s["k_scale"])), host(s["table"]), [0], [0, 5],
+                               np.zeros((5, 1, 32)))
+        with np.errstate(over="ignore"):
+            assert (host(got[0]) == want.astype(np.float32)).all()
+        check(lm, s, "f32")
+
+
+def test_what_is_out_of_range_is_left(lm):
+    """Blocks outside the pool, positions behind the table, negative lengths, offsets that fall or pass the rows;
+    rows outside the source are zeros."""
+    s = make(11, "bf16", [0, 5, 9, 12, 0], [6, 6, 6, 30, 4], 2, 32, 8, True)
+    table, rows, first = host(s["table"]), host(s["rows"]), host(s["offsets"])
+    table[0, 0], table[1, 1] = -1, 10 ** 6
+    rows[first[2]:first[2] + 2] = (-1, 10 ** 6)
+    lengths = host(s["lengths"])
+    lengths[4] = -3
+    s.update(table=put(table[:, :5]), rows=put(rows), lengths=put(lengths))
+    check(lm, s, "bf16")
+    s["offsets"] = put([0, 3, 3, 5, len(rows) - 1, len(rows) + 1])
+    check(lm, s, "bf16")
+
+
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("kv,dim,block", [(4, 32, 16), (2, 128, 64), (1, 80, 20), (3, 256, 7), (8, 16, 1)])
+def test_read(lm, typ, kv, dim, block):
+    """Whole requests, parts, one token, none; rows behind the last stay; blocks and positions that are not there are 0."""
+    rng = np.random.default_rng(2)
+    lens = np.array([3 * block + 1, 1, 40, 0, 5 * block])
+    start = np.array([0, 0, 17, 0, block])
+    table, blocks = pages(rng, lens, block)
+    table[0, 1] = -3
+    (kc, ks), (vc, vs) = cache(rng, blocks, kv, block, dim, 3)
+    kc[0, 0, 0, :2] = (0x7f, 0xff)
+    first = np.concatenate([[0], np.cumsum(lens - start)])
+    n = int(first[-1]) + 4
+    start[4] = table.shape[1] * block - 2  # runs off the table
+    both = torch.full((n, 2, kv, dim), 3.0, device="cuda").to(TYPES[typ])
+    k, v = both[:, 0], both[:, 1]
+    got = lm.mca_cache8_read(k, v, codes(kc), codes(vc), put(ks, np.uint8), put(vs, np.uint8), put(table), put(start), put(first))
+    assert got[0] is k and got[1] is v
+    for g, c, sc in ((k, kc, ks), (v, vc, vs)):
+        want = olm.cache8_read(olm.cache8_values(c, sc), table, start, first, np.full((n, kv, dim), 3.0))
+        np.testing.assert_array_equal(host(g), want)
+
+
+def test_a_cache_past_four_gigabytes(lm):
+    """Blocks whose bytes lie behind 2^32, written and read."""
+    kv, dim, block = 8, 128, 64
+    blocks = (1 << 32) // (kv * dim * block) + 40
+    k_cache = torch.zeros(blocks, kv, block, dim, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    v_cache = torch.zeros(blocks, kv, block, dim, dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn)
+    ks, vs = (torch.zeros(blocks, kv, dtype=torch.uint8, device="cuda") for _ in range(2))
+    table = put([[blocks - 1, blocks - 2, 3]])
+    k = torch.randn(150, kv, dim, device="cuda").bfloat16()
+    v = torch.randn(150, kv, dim, device="cuda").bfloat16()
+    lm.mca_cache8_append(k, v, k_cache, v_cache, ks, vs, table, put([0]), put([0, 150]))
+    got = lm.mca_cache8_read(torch.zeros_like(k), torch.zeros_like(v), k_cache, v_cache, ks, vs, table, put([0]), put([0, 150]))
+    for x, y in zip(got, (k, v)):
+        lim = torch.maximum(y.double().abs() / 16, y.abs().max().double() * 2.0 ** -10 / 224)
+        assert ((x.double() - y.double()).abs() <= lim).all()
+
+
+def test_captured(lm):
+    """Replays of append and read, with eager work and other rows between them."""
+    s = make(13, "bf16", [0, 5, 30], [40, 3, 1], 2, 64, 16)
+    s["k"], s["v"] = s["k"].clone(), s["v"].clone()
+    fresh = {n: s[n].clone() for n in ("k_cache", "v_cache", "k_scale", "v_scale")}
+    n = s["k"].shape[0]
+    out = [torch.zeros(n, 2, 64, device="cuda", dtype=torch.bfloat16) for _ in range(2)]
+    def call():
+        lm.mca_cache8_append(**s)
+        lm.mca_cache8_read(*out, s["k_cache"], s["v_cache"], s["k_scale"], s["v_scale"], s["table"], s["lengths"], s["offsets"])
+    call()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in range(3):
+        for name, t in fresh.items():
+            s[name].view(torch.uint8).copy_(t.view(torch.uint8))
+        s["k"].normal_(std=1.0 + 5 * i)
+        s["v"].normal_(std=0.1 + i)
+        want = expected(s, "bf16")
+        graph.replay()
+        torch.cuda.synchronize()
+        for name, w in zip(("k_cache", "v_cache", "k_scale", "v_scale"), want):
+            assert (host(s[name]) == w).all()
+        values = olm.cache8_values(want[0], want[2])
+        assert (host(out[0]) == olm.cache8_read(values, host(s["table"]), host(s["lengths"]), host(s["offsets"]),
+                                                np.zeros((n, 2, 64)))).all()
+
+
+def test_another_stream(lm):
+    """The current stream of the tensors' device is taken."""
+    s = make(14, "f16", [0, 5], [9, 3], 2, 64, 16)
+    want = expected(s, "f16")
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        lm.mca_cache8_append(**s)
+    stream.synchronize()
+    assert (host(s["k_cache"]) == want[0]).all() and (host(s["v_scale"]) == want[3]).all()

@@ -304,8 +304,9 @@ struct Rows {
       for (int w = 0; w < VD; ++w) vf[j][w] = ok ? vf[j][w] : 0u;
     }
   }
-  // the values of the h-th 32 tokens, weighed
-  __device__ __forceinline__ void add(int h, const uint32_t (&vf)[8][VD]) {
+  // the values of the h-th 32 tokens, weighed; word d of a lane's row j of theirs is v(j, d)
+  template <class V>
+  __device__ __forceinline__ void add_words(int h, V word) {
     if constexpr (kF32) {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -313,21 +314,28 @@ struct Rows {
         for (int e = 0; e < OT; ++e)
 #pragma unroll
           for (int t = 0; t < QT; ++t)
-            o[t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[j][e]),
+            o[t][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(word(j, e)),
                                                            __uint_as_float(pw[t][2 * h + (j >> 2)][j & 3]), o[t][e], 0, 0, 0);
     } else {
 #pragma unroll
-      for (int d = 0; d < VD; ++d)
+      for (int d = 0; d < VD; ++d) {
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = word(j, d);
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
           u32x4 v;
 #pragma unroll
           for (int j = 0; j < 4; ++j)  // tokens 2 j and 2 j + 1, the low or high half of word d
-            v[j] = __builtin_amdgcn_perm(vf[2 * j + 1][d], vf[2 * j][d], b ? 0x07060302u : 0x05040100u);
+            v[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], b ? 0x07060302u : 0x05040100u);
 #pragma unroll
           for (int t = 0; t < QT; ++t) o[t][2 * d + b] = mma32<TYPE>(v, pw[t][h], o[t][2 * d + b]);
         }
+      }
     }
+  }
+  __device__ __forceinline__ void add(int h, const uint32_t (&vf)[8][VD]) {
+    add_words(h, [&](int j, int d) { return vf[j][d]; });
   }
   // Drafted nodes: one that some rows do not see may hold anything.  Values that
   // are not finite (bits of `odd`) are left out of the products and added for the
@@ -536,8 +544,11 @@ struct Share {
 // requests of 1000 to 2000, one row a head, 4 key heads of 128, bf16: 0.6 GB in
 // 131 us).  Small calls are bound by the chain of table entry, K, scores, V (64 drafts
 // of up to 8 nodes over at most 120 tokens, 4 heads of 32, fp32: 8.5 us).
+constexpr int resident8(int type, int dp) {
+  return dp <= 64 ? (type == MCA_TYPE_F32 ? 3 : 4) : (dp <= 128 ? (type == MCA_TYPE_F32 ? 2 : 3) : 1);
+}
 template <int TYPE, int DP, bool PAD, bool C8>
-__global__ __launch_bounds__(kAttnThreads) void k_lm_attn(AttnDev p) {
+__global__ __launch_bounds__(kAttnThreads, C8 ? resident8(TYPE, DP) : 1) void k_lm_attn(AttnDev p) {
   constexpr int LB = DP / 4 < 16 ? DP / 4 : 16;  // bytes of a load of 8-bit keys
   typedef Rows<TYPE, DP, 1, 1, PAD, C8 ? LB : 0> R;
   constexpr int EL = R::EL, KL = R::KL, VD = R::VD, CD = R::CD, NC = R::NC, OT = R::OT;
@@ -656,29 +667,25 @@ __global__ __launch_bounds__(kAttnThreads) void k_lm_attn(AttnDev p) {
           w.score(x, [&](int i) { return wide_part<TYPE>(&kc[x][i / PP][i % PP * PC], f); });
         }
         w.weigh(valid == 0xffffffffu, see);
+        float f[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float f = scale_of((uint32_t)__shfl(vsc, 4 * q + (j & 3) + 16 * (j >> 2), 64));
+          f[j] = scale_of((uint32_t)__shfl(vsc, 4 * q + (j & 3) + 16 * (j >> 2), 64));
+          if (valid != 0xffffffffu) {
+            const bool ok = (valid >> (4 * q + (j & 3) + 16 * (j >> 2))) & 1;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            if constexpr (TYPE == MCA_TYPE_F32) {
-              const u32x2 lo = wide2_f32<false>(vc[j][c][0], f);
-              vf[j][c * CD] = lo[0];
-              vf[j][c * CD + 1] = lo[1];
-              if constexpr (CD == 4) {
-                const u32x2 hi = wide2_f32<true>(vc[j][c][0], f);
-                vf[j][c * CD + 2] = hi[0];
-                vf[j][c * CD + 3] = hi[1];
-              }
-            } else {
+            for (int c = 0; c < NC; ++c)
 #pragma unroll
-              for (int d = 0; d < CD; ++d)
-                vf[j][c * CD + d] = d & 1 ? wide2<TYPE, true>(vc[j][c][d / 2], f) : wide2<TYPE, false>(vc[j][c][d / 2], f);
-            }
+              for (int d = 0; d < VW; ++d) vc[j][c][d] = ok ? vc[j][c][d] : 0u;
           }
         }
-        if (valid != 0xffffffffu) w.clear(vf, valid);
-        w.add(0, vf);
+        w.add_words(0, [&](int j, int d) {
+          const int c = d / CD, x = d % CD;
+          if constexpr (TYPE == MCA_TYPE_F32)
+            return x & 2 ? wide2_f32<true>(vc[j][c][0], f[j])[x & 1] : wide2_f32<false>(vc[j][c][0], f[j])[x & 1];
+          else
+            return x & 1 ? wide2<TYPE, true>(vc[j][c][x / 2], f[j]) : wide2<TYPE, false>(vc[j][c][x / 2], f[j]);
+        });
       }
     } else {
       for (; p0 < end; p0 += kAttnWaves * kTilePos) {
@@ -1265,10 +1272,12 @@ bool big_rows(const mca_tree_attention_args& a) { return a.head_dim > (a.dtype =
 // 100000, 4 key heads, 4 rows 557 and 484, at 128 270 and 245); and many fp32 rows over
 // short contexts are too little for the wide kernel (16 of 1024, 256 rows, head_dim 64 91
 // and 65, 32 52 and 35; of 2048, 64 100 and 116).
+template <bool C8>
 bool is_wide(const mca_tree_attention_args& a) {
   const int rows = shared_rows(a);
   const int64_t pairs = (int64_t)a.n_req * a.n_kv_head, reads = pairs * ((int64_t)a.max_len + a.max_nodes);
   if (a.dtype == MCA_TYPE_F32 && !big_rows(a) && rows <= 32) return false;
+  if (C8 && rows <= 16) return false;
   if (rows <= 16) return a.max_len >= (1 << 14) && reads >= (1 << 22);
   return reads * ((rows + 15) / 16) > (pairs >= kCUs ? 3 << 17 : 5 << 17);
 }
@@ -1282,30 +1291,34 @@ int row_group(const mca_tree_attention_args& a) { return big_rows(a) || shared_r
 // head_dim 128, 64 requests of 8192: 256 rows 346 us against 389, 512 623 against 727,
 // but 128 279 against 235, 384 567 against 580; fp16, head_dim 64: 256 rows 225
 // against 229, 128 184 against 133).  Wider fp32 rows leave no registers for eight.
+template <bool C8>
 int wide_waves(const mca_tree_attention_args& a) {
   const int rows = shared_rows(a), tiles = (rows + 255) / 256;
   if (big_rows(a)) return rows > 64 && (a.dtype != MCA_TYPE_F32 || a.head_dim <= 128) ? 8 : 4;
   return a.dtype != MCA_TYPE_F32 && a.head_dim > 64 && 8 * rows >= 7 * 256 * tiles ? 8 : 4;
 }
 // rows of a workgroup, and the tokens of the wide kernel's tiles
-int tile_rows(const mca_tree_attention_args& a) { return is_wide(a) ? 16 * row_group(a) * wide_waves(a) : 16; }
+template <bool C8>
+int tile_rows(const mca_tree_attention_args& a) { return is_wide<C8>(a) ? 16 * row_group(a) * wide_waves<C8>(a) : 16; }
 int tile_tokens(const mca_tree_attention_args& a) {
   const int el = a.dtype == MCA_TYPE_F32 ? 4 : 2, d = a.head_dim <= 32 ? 32 : (a.head_dim <= 64 ? 64 : (a.head_dim <= 128 ? 128 : 256));
   return d * el <= 256 ? 64 : 32;
 }
-int row_tiles(const mca_tree_attention_args& a) { return (shared_rows(a) + tile_rows(a) - 1) / tile_rows(a); }
-int64_t wide_items(const mca_tree_attention_args& a) { return (int64_t)row_tiles(a) * a.n_kv_head * a.n_req; }
+template <bool C8>
+int row_tiles(const mca_tree_attention_args& a) { return (shared_rows(a) + tile_rows<C8>(a) - 1) / tile_rows<C8>(a); }
+template <bool C8>
+int64_t wide_items(const mca_tree_attention_args& a) { return (int64_t)row_tiles<C8>(a) * a.n_kv_head * a.n_req; }
 
 template <int TYPE, int DP, bool PAD, bool C8>
 void launch_pad(const AttnDev& p, dim3 grid, hipStream_t s) {
   constexpr bool kBig = DP > (TYPE == MCA_TYPE_F32 ? 64 : 128);             // big_rows()
   constexpr bool kEight = TYPE == MCA_TYPE_F32 ? DP == 128 : DP >= 128;     // wide_waves() may be 8
-  if (!is_wide(p.a)) {
+  if (!is_wide<C8>(p.a)) {
     hipLaunchKernelGGL((k_lm_attn<TYPE, DP, PAD, C8>), grid, dim3(kAttnThreads), 0, s, p);
     return;
   }
   if constexpr (kEight)
-    if (wide_waves(p.a) == 8) {
+    if (wide_waves<C8>(p.a) == 8) {
       hipLaunchKernelGGL((k_lm_attn_wide<TYPE, DP, kBig ? 1 : 2, 8, PAD, C8>), grid, dim3(512), 0, s, p);
       return;
     }
@@ -1327,7 +1340,7 @@ void launch_dim(const AttnDev& p, dim3 grid, hipStream_t s) {
 // (with the attention, 16 and 4 waves: one request of 60000, 64 rows, 4 key heads, bf16,
 // head_dim 128, 64 workgroups, 48 and 51 us, head_dim 256 89 and 115; 4 requests of
 // 8192, 128 rows, head_dim 128, 512 workgroups, 58 and 54).
-template <int TYPE, int NI>
+template <int TYPE, int NI, bool C8>
 void launch_join(const AttnDev& p, dim3 groups, int fours, hipStream_t s) {
   if (groups.x <= kCUs)
     hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 16>), groups, dim3(1024), 0, s, p, tile_tokens(p.a), fours);
@@ -1352,15 +1365,57 @@ void launch_type(const AttnDev& p, dim3 grid, hipStream_t s) {
     // 16 rows a workgroup once that fills the chip (what they read first they read
     // once), else 4 (64 requests of 4096, 128 rows, bf16, head_dim 128: 150 us against
     // 162 of attention and joining; one of 60000: 81 against 66)
-    const int fours = wide_items(p.a) * p.rows / 16 >= 4 * kCUs ? 4 : 1;
-    const dim3 groups((unsigned)(wide_items(p.a) * (p.rows / (4 * fours))));
+    const int fours = wide_items<C8>(p.a) * p.rows / 16 >= 4 * kCUs ? 4 : 1;
+    const dim3 groups((unsigned)(wide_items<C8>(p.a) * (p.rows / (4 * fours))));
     if (D <= 64)
-      launch_join<TYPE, 1>(p, groups, fours, s);
+      launch_join<TYPE, 1, C8>(p, groups, fours, s);
     else if (D <= 128)
-      launch_join<TYPE, 2>(p, groups, fours, s);
+      launch_join<TYPE, 2, C8>(p, groups, fours, s);
     else
-      launch_join<TYPE, 4>(p, groups, fours, s);
+      launch_join<TYPE, 4, C8>(p, groups, fours, s);
   }
+}
+
+template <bool C8>
+AttnPlan attention_plan(const mca_tree_attention_args& a) {
+  AttnPlan p{};
+  if (a.n_req == 0) return p;
+  const int64_t wgs = (int64_t)row_tiles<C8>(a) * a.n_kv_head * a.n_req;
+  if (is_wide<C8>(a)) {
+    // Shared, if that saves more than the joining costs.  A workgroup for each tile of
+    // rows takes as many rounds of `tiles` as the chip needs for them all; shared, a
+    // part of a round counts as such.  An fp32 tile counts twice, as its products do.
+    // The joining costs about the time of 12 tiles and of the parts, two a workgroup.
+    // (128 rows, 4 key heads, bf16, head_dim 128, shared and not: one request of 512
+    // tokens 33 and 28 us, of 1024 33 and 41; 16 of 1024 52 and 43, of 2048 58 and 71;
+    // 64 of 4096 147 and 133, of 16384 380 and 464.)
+    const bool one = wide_waves<C8>(a) == 8 || (a.dtype == MCA_TYPE_F32 && a.head_dim > 128);  // LDS or registers of a CU
+    const int tokens = tile_tokens(a), resident = kCUs * (one ? 1 : 2);
+    const int64_t tiles = (a.max_len + tokens - 1) / tokens;
+    p.chunk = a.max_len;
+    p.splits = 1;
+    const int64_t idle = (wgs + resident - 1) / resident * resident - wgs;
+    const bool saves = (a.dtype == MCA_TYPE_F32 ? 2 : 1) * tiles * idle / resident > 12 + std::min<int64_t>(wgs, resident) / 8;
+    if (saves && wgs * (tiles + MCA_MAX_NODES / 32) < (1 << 30)) {
+      p.sharers = (int32_t)std::min<int64_t>(resident, (wgs * (tiles + MCA_MAX_NODES / 32) / kLeastUnits + 8) / 8 * 8);
+      p.bytes = ((size_t)a.n_req + 1 + 63) / 64 * 256 + (size_t)2 * p.sharers * tile_rows<C8>(a) * (a.head_dim + 1) * sizeof(float);
+    }
+    return p;
+  }
+  // Chunks of at least two tiles a wave while there are fewer than two workgroups a
+  // CU; behind that of 1536 tokens, up to 16 workgroups a CU, which evens out requests
+  // of different lengths.  (Workgroups in all of 512, 1024, 2048 and 4096, bf16,
+  // head_dim 128, 8 key heads: one request of 200000 162, 170, 185 and 185 us; 32 of
+  // 8192 to 32768 526, 500, 478 and 470.)
+  const int64_t step = kAttnWaves * kTilePos;
+  const int64_t first = std::min<int64_t>((512 + wgs - 1) / wgs, (a.max_len + 2 * step - 1) / (2 * step));
+  const int64_t more = std::min<int64_t>((4096 + wgs - 1) / wgs, (a.max_len + 1535) / 1536);
+  const int64_t want = std::clamp<int64_t>(std::max(first, more), 1, 256);
+  const int64_t chunk = (a.max_len + want - 1) / want;
+  p.chunk = (int32_t)std::max<int64_t>(step, (chunk + step - 1) / step * step);
+  p.splits = (int32_t)std::max<int64_t>(1, ((int64_t)a.max_len + p.chunk - 1) / p.chunk);
+  p.bytes = p.splits > 1 ? (size_t)a.n_rows * a.n_head * p.splits * (a.head_dim + 1) * sizeof(float) : 0;
+  return p;
 }
 
 template <bool C8>
@@ -1370,11 +1425,11 @@ hipError_t launch_attention(const mca_tree_attention_args& a, const AttnPlan& pl
   AttnDev p;
   p.a = a;
   p.group = a.n_head / a.n_kv_head;
-  p.row_tiles = row_tiles(a);
+  p.row_tiles = row_tiles<C8>(a);
   p.chunk = plan.chunk;
   p.splits = plan.splits;
   p.sharers = plan.sharers;
-  p.rows = tile_rows(a);
+  p.rows = tile_rows<C8>(a);
   p.first_unit = (int32_t*)a.workspace;
   p.part_o = (float*)a.workspace;
   size_t parts = (size_t)a.n_rows * a.n_head * plan.splits;

@@ -3,7 +3,7 @@
 
 namespace mca {
 
-AttnPlan lm_attention8_plan(const mca_tree_attention8_args& a) { return lm_attention_plan(a.of); }
+AttnPlan lm_attention8_plan(const mca_tree_attention8_args& a) { return attention_plan<true>(a.of); }
 
 hipError_t lm_launch_attention8(const mca_tree_attention8_args& a, const AttnPlan& plan, hipStream_t s) {
   return launch_attention<true>(a.of, plan, a.k_scale, a.v_scale, s);

@@ -23,9 +23,14 @@ namespace {
 
 constexpr int kVThreads = 256;
 constexpr int kVWaves = kVThreads / 64;
+constexpr int kWalkThreads = 1024;  // of the walk over large vocabularies, whose passes one workgroup makes
 constexpr int kVUnroll = 4;
 constexpr int kVMaxSplits = 64;   // parts of a row
 constexpr int64_t kVPart = 8192;  // symbols of a part at least
+constexpr int kVSide = 8;         // symbols side by side in a thread of the draw
+constexpr int kVCut = 4096;       // symbols of a cut of the draw, but for very large vocabularies
+// Largest vocabulary of the kernel that does all of a request in one workgroup.
+constexpr int kVSmall = 1024;
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -54,6 +59,37 @@ struct VerifyDev {
   int32_t* paths;        // [n_rows]
 };
 
+// exp(x) of N numbers x <= 0, to 2^-47: 2^n times the series of exp in the rest, which is
+// at most ln 2 / 2, to its 11th power.  Results below 2^-1022 are 0, NaN stays.
+// The steps of several go side by side: one by one, each would wait for the one before.
+template <int N>
+__device__ __forceinline__ void exps_of(double (&x)[N]) {
+  constexpr double kInvLn2 = 1.4426950408889634074, kLn2 = 0.69314718055994530942, kLn2Rest = 2.3190468138462996e-17;
+  constexpr double kOver[12] = {1.0,          1.0,           1.0 / 2,        1.0 / 6,         1.0 / 24,         1.0 / 120,
+                                1.0 / 720,    1.0 / 5040,    1.0 / 40320,    1.0 / 362880,    1.0 / 3628800,    1.0 / 39916800};  // 1 / k!
+  double n[N], r[N], y[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) n[i] = __builtin_rint(x[i] * kInvLn2);
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = fma(n[i], -kLn2, x[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = fma(n[i], -kLn2Rest, r[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) y[i] = kOver[11];
+#pragma unroll
+  for (int k = 10; k >= 0; --k) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = fma(y[i], r[i], kOver[k]);
+    if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = x[i] < -708.0 ? 0.0 : __builtin_ldexp(y[i], (int)n[i]);
+}
+__device__ __forceinline__ double exp_of(double x) {
+  double y[1] = {x};
+  exps_of(y);
+  return y[0];
+}
 // 16 bytes at any address
 template <int TYPE>
 __device__ __forceinline__ void load_any(const char* p, float (&f)[Elem<TYPE>::kPer]) {
@@ -222,95 +258,92 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_rows(VerifyDev p) {
   }
 }
 
-// A request's walk, by one workgroup; every wave takes the same steps.
-template <int TYPE, bool GREEDY>
-__global__ __launch_bounds__(kVThreads) void k_lm_verify_walk(VerifyDev p) {
-  constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
-  typedef typename Elem<TYPE>::Raw Raw;
-  const mca_verify_drafts_args& a = p.a;
-  const bool drawn = a.draft != nullptr && !GREEDY;
-  __shared__ float s_m[2][MCA_MAX_NODES];
-  __shared__ double s_sum[2][MCA_MAX_NODES];  // 0: no softmax; of greedy calls 1
-  __shared__ int s_best[MCA_MAX_NODES];
-  __shared__ int s_up[MCA_MAX_NODES], s_tok[MCA_MAX_NODES];
-  __shared__ float s_u[MCA_MAX_NODES];
-  __shared__ double s_p[MCA_MAX_NODES], s_q[MCA_MAX_NODES];  // of a node's token at its parent
-  __shared__ double s_red[kVWaves];
-  const int tid = threadIdx.x, lane = tid & 63, r = blockIdx.x, V = (int)a.n_vocab;
-  int first, n;
-  if (tid == 0) p.tickets[r] = 0;
-  if (!nodes_of(a, r, &first, &n)) {
-    if (tid == 0) {
-      a.new_len[r] = a.lengths[r];
-      a.token[r] = -1;
-      p.ends[r].row = -1;
-    }
-    return;
-  }
-  // every node's sums, parent and token
-  for (int x = tid; x < n * (drawn ? 2 : 1); x += kVThreads) {
-    const int which = x >= n, i = x - which * n;
-    const RowPart* part = p.parts + ((int64_t)(first + i) * (drawn ? 2 : 1) + which) * p.splits;
-    bool parent = which == 0;
-    if (which)
-      for (int j = i + 1; j < n; ++j) parent = parent || a.parents[first + j] == i;
-    float m = kLowest;
-    double s = 0;
-    int at = -1;
-    if (GREEDY) m = -__builtin_huge_valf();
-    if (parent) {
-      for (int y = 0; y < p.splits; ++y) {
-        const RowPart u = part[y];
-        if constexpr (GREEDY) {
-          if (u.m > m) {
-            m = u.m;
-            at = u.at;
-          }
-          s += u.s;
-        } else {
-          m = fmaxf(m, u.m);
-        }
-      }
-      if constexpr (GREEDY) {
-        s = s == 0 && at >= 0 ? 1.0 : 0.0;
-      } else {
-        const double k = which ? a.draft_scale : a.scale;
-        for (int y = 0; y < p.splits; ++y) s += (double)part[y].s * exp(k * ((double)part[y].m - (double)m));
-      }
-    }
-    s_m[which][i] = m;
-    s_sum[which][i] = s > 0 ? s : 0.0;  // NaN: none
-    if (which == 0) s_best[i] = at;
-  }
+namespace {
+
+// What a walk needs of its nodes, in LDS.
+struct Nodes {
+  float m[2][MCA_MAX_NODES];      // largest logits of the target and the draft
+  double sum[2][MCA_MAX_NODES];   // 0: no softmax; of greedy calls 1
+  int best[MCA_MAX_NODES];        // of greedy calls the first symbol of the largest logit
+  int up[MCA_MAX_NODES], tok[MCA_MAX_NODES];
+  float u[MCA_MAX_NODES];
+  double p[MCA_MAX_NODES], q[MCA_MAX_NODES];  // of a node's token at its parent
+  uint8_t parent[MCA_MAX_NODES];  // whether a node has children
+  double red[kWalkThreads / 64];
+};
+
+// Parents, tokens and random numbers of a request's nodes (THREADS >= MCA_MAX_NODES).
+template <bool GREEDY>
+__device__ __forceinline__ void load_nodes(const mca_verify_drafts_args& a, int first, int n, Nodes& s) {
+  const int tid = threadIdx.x;
+  int up = -1;
   if (tid < n) {
-    const int up = a.parents[first + tid];
-    s_up[tid] = tid > 0 && up >= 0 && up < tid ? up : -1;
-    s_tok[tid] = a.tokens[first + tid];
-    if constexpr (!GREEDY) s_u[tid] = a.accept[first + tid];
+    up = a.parents[first + tid];
+    up = tid > 0 && up >= 0 && up < tid ? up : -1;
+    s.up[tid] = up;
+    s.tok[tid] = a.tokens[first + tid];
+    if constexpr (!GREEDY) s.u[tid] = a.accept[first + tid];
+    s.parent[tid] = 0;
   }
   __syncthreads();
-  if (!GREEDY && tid < n && s_up[tid] >= 0 && s_tok[tid] >= 0 && s_tok[tid] < V) {
-    const int up = s_up[tid];
+  if (up >= 0) s.parent[up] = 1;
+}
+
+// The sum of max(p - c q, 0) over the vocabulary at a node.
+template <int TYPE, int THREADS>
+__device__ __forceinline__ double left_sum(const mca_verify_drafts_args& a, int first, int node, double c, Nodes& s) {
+  constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
+  const int V = (int)a.n_vocab;
+  const char* zt = (const char*)a.target + (first + node) * a.target_row * EL;
+  const char* zd = (const char*)a.draft + (first + node) * a.draft_row * EL;
+  const float mp = s.m[0][node], mq = s.m[1][node];
+  const float kp = (float)a.scale * kLog2e, kq = (float)a.draft_scale * kLog2e;
+  // logarithms (base 2) of the factors of the exponentials
+  const float fp = -__builtin_amdgcn_logf((float)s.sum[0][node]), fq = __builtin_amdgcn_logf((float)(c / s.sum[1][node]));
+  double mine = 0;
+#pragma unroll 4
+  for (int v = threadIdx.x * VE; v < V; v += THREADS * VE) {
+    float x[VE], y[VE], w = 0.f;
+    load_symbols<TYPE>(zt, v, V, x);
+    load_symbols<TYPE>(zd, v, V, y);
+#pragma unroll
+    for (int e = 0; e < VE; ++e)
+      w += fmaxf(__builtin_amdgcn_exp2f(fmaf(x[e] - mp, kp, fp)) - __builtin_amdgcn_exp2f(fmaf(y[e] - mq, kq, fq)), 0.f);
+    mine += (double)w;
+  }
+  return group_sum<THREADS / 64>(mine, s.red);
+}
+
+// A request's walk, by one workgroup, whose waves all take the same steps; s.m, s.sum
+// and s.best are there.  Writes the path and new_len, and the token where no draw follows.
+template <int TYPE, bool GREEDY, int THREADS>
+__device__ __forceinline__ End walk(const VerifyDev& d, int r, int first, int n, Nodes& s) {
+  typedef typename Elem<TYPE>::Raw Raw;
+  const mca_verify_drafts_args& a = d.a;
+  const bool drawn = a.draft != nullptr && !GREEDY;
+  const int tid = threadIdx.x, lane = tid & 63, V = (int)a.n_vocab;
+  if (!GREEDY && tid < n && s.up[tid] >= 0 && s.tok[tid] >= 0 && s.tok[tid] < V) {
+    const int up = s.up[tid];
     const int64_t row = first + up;
-    const float z = to_f32<TYPE>(((const Raw*)a.target)[row * a.target_row + s_tok[tid]]);
-    s_p[tid] = exp(a.scale * ((double)z - (double)s_m[0][up])) / s_sum[0][up];
+    const float z = to_f32<TYPE>(((const Raw*)a.target)[row * a.target_row + s.tok[tid]]);
+    s.p[tid] = exp_of(a.scale * ((double)z - (double)s.m[0][up])) / s.sum[0][up];
     if (drawn) {
-      const float d = to_f32<TYPE>(((const Raw*)a.draft)[row * a.draft_row + s_tok[tid]]);
-      s_q[tid] = exp(a.draft_scale * ((double)d - (double)s_m[1][up])) / s_sum[1][up];
+      const float y = to_f32<TYPE>(((const Raw*)a.draft)[row * a.draft_row + s.tok[tid]]);
+      s.q[tid] = exp_of(a.draft_scale * ((double)y - (double)s.m[1][up])) / s.sum[1][up];
     }
   }
   __syncthreads();
-  const int up0 = lane < n ? s_up[lane] : -1, up1 = lane + 64 < n ? s_up[lane + 64] : -1;
-  const bool legal0 = lane < n && s_tok[lane] >= 0 && s_tok[lane] < V;
-  const bool legal1 = lane + 64 < n && s_tok[lane + 64] >= 0 && s_tok[lane + 64] < V;
+  const int up0 = lane < n ? s.up[lane] : -1, up1 = lane + 64 < n ? s.up[lane + 64] : -1;
+  const bool legal0 = lane < n && s.tok[lane] >= 0 && s.tok[lane] < V;
+  const bool legal1 = lane + 64 < n && s.tok[lane + 64] >= 0 && s.tok[lane + 64] < V;
   int node = 0, count = 1, gone = 0;
   double c = 0;
   bool ok = true;
-  if (tid == 0) p.paths[first] = first;
+  if (tid == 0) d.paths[first] = first;
   while (true) {
     // its children in their order
     uint64_t kids[2] = {__ballot(up0 == node), __ballot(up1 == node)};
-    ok = s_sum[0][node] > 0 && (!drawn || (kids[0] | kids[1]) == 0 || s_sum[1][node] > 0);
+    ok = s.sum[0][node] > 0 && (!drawn || (kids[0] | kids[1]) == 0 || s.sum[1][node] > 0);
     if (!ok) break;
     kids[0] &= __ballot(legal0);
     kids[1] &= __ballot(legal1);
@@ -323,40 +356,23 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_walk(VerifyDev p) {
       if (i < 0) break;
       if (i < 64) kids[0] &= kids[0] - 1; else kids[1] &= kids[1] - 1;
       if constexpr (GREEDY) {
-        if (s_tok[i] == s_best[node]) {
+        if (s.tok[i] == s.best[node]) {
           go = i;
           break;
         }
       } else if (drawn) {
-        if ((double)s_u[i] * sum * s_q[i] < s_p[i] - c * s_q[i]) {
+        if ((double)s.u[i] * sum * s.q[i] < s.p[i] - c * s.q[i]) {
           go = i;
           break;
         }
         c += sum;
-        if (kids[0] | kids[1]) {
-          const char* zt = (const char*)a.target + (first + node) * a.target_row * EL;
-          const char* zd = (const char*)a.draft + (first + node) * a.draft_row * EL;
-          const float mp = s_m[0][node], mq = s_m[1][node];
-          const float kp = (float)a.scale * kLog2e, kq = (float)a.draft_scale * kLog2e;
-          const float fp = (float)(1.0 / s_sum[0][node]), fq = (float)(c / s_sum[1][node]);
-          double mine = 0;
-          for (int v = tid * VE; v < V; v += kVThreads * VE) {
-            float x[VE], y[VE], w = 0.f;
-            load_symbols<TYPE>(zt, v, V, x);
-            load_symbols<TYPE>(zd, v, V, y);
-#pragma unroll
-            for (int e = 0; e < VE; ++e)
-              w += fmaxf(fmaf(__builtin_amdgcn_exp2f((x[e] - mp) * kp), fp, -(__builtin_amdgcn_exp2f((y[e] - mq) * kq) * fq)), 0.f);
-            mine += (double)w;
-          }
-          sum = group_sum<kVWaves>(mine, s_red);
-        }
+        if (kids[0] | kids[1]) sum = left_sum<TYPE, THREADS>(a, first, node, c, s);
       } else {
         // a symbol that was rejected before has nothing left
         bool again = false;
-        for (int j = node + 1; j < i; ++j) again = again || (s_up[j] == node && s_tok[j] == s_tok[i]);
-        const double left = again ? 0.0 : s_p[i];
-        if ((double)s_u[i] * sum < left) {
+        for (int j = node + 1; j < i; ++j) again = again || (s.up[j] == node && s.tok[j] == s.tok[i]);
+        const double left = again ? 0.0 : s.p[i];
+        if ((double)s.u[i] * sum < left) {
           go = i;
           break;
         }
@@ -366,53 +382,265 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_walk(VerifyDev p) {
     }
     if (go < 0) break;
     node = go;
-    if (tid == 0) p.paths[first + count] = first + node;
+    if (tid == 0) d.paths[first + count] = first + node;
     ++count;
   }
   if (tid == 0) {
     a.new_len[r] = a.lengths[r] + count;
-    a.token[r] = GREEDY && ok ? s_best[node] : -1;
-    p.ends[r] = {ok && !GREEDY ? first + (int64_t)node : -1, c, s_m[0][node], drawn ? s_m[1][node] : 0.f, first, node, gone, 0};
+    if (GREEDY || !ok) a.token[r] = ok ? s.best[node] : -1;
   }
+  return {ok && !GREEDY ? first + (int64_t)node : -1, c, s.m[0][node], drawn ? s.m[1][node] : 0.f, first, node, gone, 0};
+}
+// of a request that has no nodes, or too many
+__device__ __forceinline__ void no_walk(const mca_verify_drafts_args& a, int r) {
+  a.new_len[r] = a.lengths[r];
+  a.token[r] = -1;
+}
+
+// What the token is drawn from: ip times exp(scale (z - mp)) less iq times the draft's, or
+// none of some symbols.
+struct Weights {
+  const char *zt, *zd;
+  double k, kd, mp, mq, ip, iq;
+  const int* gone;  // in LDS
+  int n_gone;
+};
+// Of given drafts, the symbols that were rejected at the node, to LDS (all threads).
+__device__ __forceinline__ int gone_symbols(const mca_verify_drafts_args& a, const End& e, int* s_gone, int* s_count) {
+  if (e.gone == 0) return 0;
+  if (threadIdx.x == 0) *s_count = 0;
+  __syncthreads();
+  const int j = e.node + 1 + (int)threadIdx.x;
+  if (j < e.gone && a.parents[e.first + j] == e.node) s_gone[atomicAdd(s_count, 1)] = a.tokens[e.first + j];
+  __syncthreads();
+  return *s_count;
+}
+template <int TYPE>
+__device__ __forceinline__ Weights weights_of(const mca_verify_drafts_args& a, const End& e, double sp, double sq, const int* gone, int n_gone) {
+  constexpr int EL = Elem<TYPE>::kSize;
+  return {(const char*)a.target + e.row * a.target_row * EL,
+          (const char*)a.draft + (a.draft != nullptr ? e.row * a.draft_row * EL : 0),
+          a.scale, a.draft_scale, (double)e.mp, (double)e.mq, e.c != 0 ? 1 / sp : 1.0, e.c != 0 ? e.c / sq : 0.0, gone, n_gone};
+}
+// The E symbols of a thread from v on, below hi (behind it -inf).
+template <int TYPE, int E>
+__device__ __forceinline__ void symbols(const char* row, int v, int hi, float (&x)[E]) {
+  typedef typename Elem<TYPE>::Raw Raw;
+  struct __attribute__((packed)) Any {
+    Raw x[E];
+  };
+  if (v + E <= hi) {
+    const Any y = *(const Any*)(row + (int64_t)v * Elem<TYPE>::kSize);
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = to_f32<TYPE>(y.x[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = v + i < hi ? to_f32<TYPE>(((const Raw*)row)[v + i]) : -__builtin_huge_valf();
+  }
+}
+// their weights; `plain`: of p alone
+template <int TYPE, int E>
+__device__ __forceinline__ void weigh(const Weights& f, int v, int hi, bool plain, double (&w)[E]) {
+  const bool both = f.iq != 0 && !plain;
+  float x[E], y[E];
+  symbols<TYPE, E>(f.zt, v, hi, x);
+  if (both) symbols<TYPE, E>(f.zd, v, hi, y);
+#pragma unroll
+  for (int i = 0; i < E; ++i) w[i] = 0;
+#pragma unroll 1
+  for (int which = 0; which < (both ? 2 : 1); ++which) {
+    const double k = which ? f.kd : f.k, m = which ? f.mq : f.mp, by = which ? -f.iq : f.ip;
+    double e[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) e[i] = k * ((double)(which ? y[i] : x[i]) - m);
+    exps_of(e);
+#pragma unroll
+    for (int i = 0; i < E; ++i) w[i] += e[i] * by;  // (both products rounded: equal ones leave nothing)
+  }
+#pragma unroll
+  for (int i = 0; i < E; ++i) w[i] = w[i] < 0 ? 0.0 : w[i];
+  if (!plain)
+    for (int j = 0; j < f.n_gone; ++j) {
+      const int out = f.gone[j] - v;
+#pragma unroll
+      for (int i = 0; i < E; ++i) w[i] = i == out ? 0.0 : w[i];
+    }
+}
+template <int TYPE, int E>
+__device__ __forceinline__ double weight_sum(const Weights& f, int lo, int hi, bool plain, double* s_red) {
+  double mine = 0;
+#pragma unroll 1
+  for (int v = lo + (int)threadIdx.x * E; v < hi; v += kVThreads * E) {
+    double w[E];
+    weigh<TYPE, E>(f, v, hi, plain, w);
+#pragma unroll
+    for (int i = 0; i < E; ++i) mine += w[i];
+  }
+  return group_sum<kVWaves>(mine, s_red);
+}
+// The sums of both softmaxes' exponentials over symbols lo .. hi - 1.
+template <int TYPE, int E>
+__device__ __forceinline__ void exp_sums(const Weights& f, int lo, int hi, double* s_red, double* sp, double* sq) {
+  double sum[2] = {0, 0};
+#pragma unroll 1
+  for (int v = lo + (int)threadIdx.x * E; v < hi; v += kVThreads * E) {
+    float x[E], y[E];
+    symbols<TYPE, E>(f.zt, v, hi, x);
+    symbols<TYPE, E>(f.zd, v, hi, y);
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+      const double k = which ? f.kd : f.k, m = which ? f.mq : f.mp;
+      double e[E], mine = 0;
+#pragma unroll
+      for (int i = 0; i < E; ++i) e[i] = k * ((double)(which ? y[i] : x[i]) - m);
+      exps_of(e);
+#pragma unroll
+      for (int i = 0; i < E; ++i) mine += e[i];
+      sum[0] += which ? 0.0 : mine;
+      sum[1] += which ? mine : 0.0;
+    }
+  }
+  *sp = group_sum<kVWaves>(sum[0], s_red);
+  *sq = group_sum<kVWaves>(sum[1], s_red);
+}
+
+__device__ __forceinline__ double goal_of(const mca_verify_drafts_args& a, int r, double total) {
+  const float u = a.sample[r];
+  return (u >= 0.f ? (double)fminf(u, 0x1.fffffep-1f) : 0.0) * total;
+}
+// Of the workgroup's next symbols, E side by side in a thread from v0 on, with weights w:
+// the first with which the sum, *before in front of them, is past the goal; 0x7fffffff if
+// none is.  *before moves behind them, *last becomes the thread's last of any weight.
+template <int E>
+__device__ __forceinline__ int past_goal(const double (&w)[E], int v0, double goal, double* before, int* last, double* s_wave, int* s_found) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  double mine = 0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    mine += w[i];
+    if (w[i] > 0) *last = v0 + i;
+  }
+  double run = mine;
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) {
+    const double up = __shfl_up(run, x, 64);
+    if (lane >= x) run += up;
+  }
+  __syncthreads();
+  if (lane == 63) s_wave[wave] = run;
+  if (tid == 0) *s_found = 0x7fffffff;
+  __syncthreads();
+  double at = *before;
+#pragma unroll
+  for (int x = 0; x < kVWaves; ++x) {
+    if (x < wave) at += s_wave[x];
+    *before += s_wave[x];
+  }
+  at += run - mine;
+  int mark = 0x7fffffff;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    at += w[i];
+    if (w[i] > 0 && at > goal) mark = min(mark, v0 + i);
+  }
+  if (mark != 0x7fffffff) atomicMin(s_found, mark);
+  __syncthreads();
+  return *s_found;
+}
+// Where only the rounding of the sums leaves none: the last of any weight (-1: none has).
+__device__ __forceinline__ int last_of(int last, int* s_found) {
+  __syncthreads();
+  if (threadIdx.x == 0) *s_found = -1;
+  __syncthreads();
+  atomicMax(s_found, last);
+  __syncthreads();
+  return *s_found;
+}
+
+}  // namespace
+
+// A request's walk over a large vocabulary, from the rows' parts.
+template <int TYPE, bool GREEDY>
+__global__ __launch_bounds__(kWalkThreads) void k_lm_verify_walk(VerifyDev d) {
+  const mca_verify_drafts_args& a = d.a;
+  const bool drawn = a.draft != nullptr && !GREEDY;
+  __shared__ Nodes s;
+  const int tid = threadIdx.x, r = blockIdx.x;
+  int first, n;
+  if (tid == 0) d.tickets[r] = 0;
+  if (!nodes_of(a, r, &first, &n)) {
+    if (tid == 0) {
+      no_walk(a, r);
+      d.ends[r].row = -1;
+    }
+    return;
+  }
+  load_nodes<GREEDY>(a, first, n, s);
+  __syncthreads();
+  for (int x = tid; x < n * (drawn ? 2 : 1); x += kWalkThreads) {
+    const int which = x >= n, i = x - which * n;
+    const RowPart* part = d.parts + ((int64_t)(first + i) * (drawn ? 2 : 1) + which) * d.splits;
+    float m = GREEDY ? -__builtin_huge_valf() : kLowest;
+    double sum = 0;
+    int at = -1;
+    if (which == 0 || s.parent[i]) {
+#pragma unroll 4
+      for (int y = 0; y < d.splits; ++y) {
+        const RowPart u = part[y];
+        if constexpr (GREEDY) {
+          if (u.m > m) {
+            m = u.m;
+            at = u.at;
+          }
+          sum += u.s;
+        } else {
+          m = fmaxf(m, u.m);
+        }
+      }
+      if constexpr (GREEDY) {
+        sum = sum == 0 && at >= 0 ? 1.0 : 0.0;
+      } else {
+        const double k = which ? a.draft_scale : a.scale;
+#pragma unroll 4
+        for (int y = 0; y < d.splits; ++y) sum += (double)part[y].s * exp_of(k * ((double)part[y].m - (double)m));
+      }
+    }
+    s.m[which][i] = m;
+    s.sum[which][i] = sum > 0 ? sum : 0.0;  // NaN: none
+    if (which == 0) s.best[i] = at;
+  }
+  __syncthreads();
+  const End e = walk<TYPE, GREEDY, kWalkThreads>(d, r, first, n, s);
+  if (tid == 0) d.ends[r] = e;
 }
 
 // Symbols of a cut of a row.
-__device__ __forceinline__ void cut_of(const VerifyDev& p, int cut, int* lo, int* hi) {
-  const int V = (int)p.a.n_vocab, per = ((V + p.cuts - 1) / p.cuts + 7) / 8 * 8;
+__device__ __forceinline__ void cut_of(const VerifyDev& d, int cut, int* lo, int* hi) {
+  const int V = (int)d.a.n_vocab, per = ((V + d.cuts - 1) / d.cuts + 7) / 8 * 8;
   *lo = (int)min((int64_t)cut * per, (int64_t)V);
-  *hi = min(V, *lo + per);
+  *hi = (int)min((int64_t)*lo + per, (int64_t)V);
 }
 
 // Where something was rejected: the sums of both softmaxes again, in 64 bits.
 template <int TYPE>
-__global__ __launch_bounds__(kVThreads) void k_lm_verify_sums(VerifyDev p) {
-  constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
-  const mca_verify_drafts_args& a = p.a;
+__global__ __launch_bounds__(kVThreads) void k_lm_verify_sums(VerifyDev d) {
   __shared__ double s_red[kVWaves];
   const int r = blockIdx.x, cut = blockIdx.y;
-  const End e = p.ends[r];
+  const End e = d.ends[r];
   if (e.row < 0 || e.c == 0) return;
   int lo, hi;
-  cut_of(p, cut, &lo, &hi);
-#pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const char* row = (const char*)(which ? a.draft : a.target) + e.row * (which ? a.draft_row : a.target_row) * EL;
-    const double k = which ? a.draft_scale : a.scale, m = which ? e.mq : e.mp;
-    double mine = 0;
-    for (int v = lo + (int)threadIdx.x * VE; v < hi; v += kVThreads * VE) {
-      float f[VE];
-      load_symbols<TYPE>(row, v, hi, f);
-#pragma unroll
-      for (int i = 0; i < VE; ++i) mine += exp(k * ((double)f[i] - m));
-    }
-    const double sum = group_sum<kVWaves>(mine, s_red);
-    if (threadIdx.x == 0) p.sums[((int64_t)r * 2 + which) * p.cuts + cut] = sum;
+  cut_of(d, cut, &lo, &hi);
+  double sp, sq;
+  exp_sums<TYPE, kVSide>(weights_of<TYPE>(d.a, e, 1, 1, nullptr, 0), lo, hi, s_red, &sp, &sq);
+  if (threadIdx.x == 0) {
+    d.sums[(int64_t)r * 2 * d.cuts + cut] = sp;
+    d.sums[((int64_t)r * 2 + 1) * d.cuts + cut] = sq;
   }
 }
 
 // The rows accepted, request after request (one workgroup).
-__device__ void compact(const VerifyDev& p, int* s_wave) {
-  const mca_verify_drafts_args& a = p.a;
+__device__ void compact(const VerifyDev& d, int* s_wave) {
+  const mca_verify_drafts_args& a = d.a;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int64_t base = 0;
   for (int r0 = 0; r0 < a.n_req; r0 += kVThreads) {
@@ -420,9 +648,9 @@ __device__ void compact(const VerifyDev& p, int* s_wave) {
     const int n = r < a.n_req ? a.new_len[r] - a.lengths[r] : 0;
     int run = n;
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(run, d, 64);
-      if (lane >= d) run += up;
+    for (int x = 1; x < 64; x <<= 1) {
+      const int up = __shfl_up(run, x, 64);
+      if (lane >= x) run += up;
     }
     if (lane == 63) s_wave[wave] = run;
     __syncthreads();
@@ -434,168 +662,195 @@ __device__ void compact(const VerifyDev& p, int* s_wave) {
     }
     const int first = n > 0 ? a.offsets[r] : 0;
     for (int i = 0; i < n; ++i)
-      if (base + pre + i < a.n_rows) a.rows[base + pre + i] = p.paths[first + i];
+      if (base + pre + i < a.n_rows) a.rows[base + pre + i] = d.paths[first + i];
     base += all;
     __syncthreads();
   }
   for (int64_t t = base + tid; t < a.n_rows; t += kVThreads) a.rows[t] = -1;
 }
 
-__global__ __launch_bounds__(kVThreads) void k_lm_verify_compact(VerifyDev p) {
+__global__ __launch_bounds__(kVThreads) void k_lm_verify_compact(VerifyDev d) {
   __shared__ int s_wave[kVWaves];
-  compact(p, s_wave);
+  compact(d, s_wave);
 }
 
 // The draw: every cut's sum of what is drawn from; the request's last workgroup finds
 // the cut, then the symbol.  Workgroup (n_req, 0) puts the rows together.
 template <int TYPE>
-__global__ __launch_bounds__(kVThreads) void k_lm_verify_draw(VerifyDev p) {
-  constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
-  const mca_verify_drafts_args& a = p.a;
-  __shared__ double s_red[kVWaves];
-  __shared__ double s_all[kVMaxSplits], s_scan[kVThreads];
-  __shared__ int s_wave[kVWaves];
+__global__ __launch_bounds__(kVThreads) void k_lm_verify_draw(VerifyDev d) {
+  const mca_verify_drafts_args& a = d.a;
+  __shared__ double s_red[kVWaves], s_all[kVMaxSplits];
+  __shared__ int s_wave[kVWaves], s_gone[MCA_MAX_NODES];
   __shared__ int s_last, s_found;
-  const int tid = threadIdx.x, r = blockIdx.x, cut = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, r = blockIdx.x, cut = blockIdx.y;
   if (r == a.n_req) {
-    if (cut == 0) compact(p, s_wave);
+    if (cut == 0) compact(d, s_wave);
     return;
   }
-  const End e = p.ends[r];
+  const End e = d.ends[r];
   if (e.row < 0) return;
-  const char* zt = (const char*)a.target + e.row * a.target_row * EL;
-  const char* zd = (const char*)a.draft + (a.draft != nullptr ? e.row * a.draft_row * EL : 0);
-  double ip = 1, iq = 0;
+  // (every wave for itself, a cut a lane)
+  double sp = 1, sq = 1;
   if (e.c != 0) {
-    double sp = 0, sq = 0;
-    for (int x = 0; x < p.cuts; ++x) {
-      sp += p.sums[((int64_t)r * 2) * p.cuts + x];
-      sq += p.sums[((int64_t)r * 2 + 1) * p.cuts + x];
-    }
-    ip = 1 / sp;
-    iq = e.c / sq;
+    const double* sums = d.sums + (int64_t)r * 2 * d.cuts;
+    sp = wave_sum(lane < d.cuts ? sums[lane] : 0.0);
+    sq = wave_sum(lane < d.cuts ? sums[d.cuts + lane] : 0.0);
   }
-  // what symbols v .. are drawn from; `plain`: from p
-  auto weights = [&](int v, int hi, bool plain, double (&w)[VE]) {
-    float x[VE];
-    load_symbols<TYPE>(zt, v, hi, x);
-#pragma unroll
-    for (int i = 0; i < VE; ++i) w[i] = exp(a.scale * ((double)x[i] - (double)e.mp)) * ip;
-    if (e.c != 0 && !plain) {
-      load_symbols<TYPE>(zd, v, hi, x);
-#pragma unroll
-      for (int i = 0; i < VE; ++i) w[i] = fmax(w[i] - iq * exp(a.draft_scale * ((double)x[i] - (double)e.mq)), 0.0);
-    }
-    if (e.gone > 0 && !plain) {
-      for (int j = e.node + 1; j < e.gone; ++j) {
-        const int out = a.tokens[e.first + j] - v;
-        if (a.parents[e.first + j] == e.node && out >= 0 && out < VE) {
-#pragma unroll
-          for (int i = 0; i < VE; ++i) w[i] = i == out ? 0.0 : w[i];
-        }
-      }
-    }
-  };
+  const Weights f = weights_of<TYPE>(a, e, sp, sq, s_gone, gone_symbols(a, e, s_gone, &s_found));
   int lo, hi;
-  cut_of(p, cut, &lo, &hi);
-  double mine = 0;
-  for (int v = lo + tid * VE; v < hi; v += kVThreads * VE) {
-    double w[VE];
-    weights(v, hi, false, w);
+  cut_of(d, cut, &lo, &hi);
+  // First this cut's sum; then, of the request's last workgroup, the cut in which the goal
+  // lies (and, where nothing is left, between them the sums of p over all cuts).  One body
+  // serves them all: nothing here runs often enough to pay for more instructions.
+  bool plain = false, finding = false;
+  int x = 0, last = -1;
+  double before = 0, goal = 0;
+  while (true) {
+    double mine = 0;
+#pragma unroll 1
+    for (int b = lo; b < hi; b += kVThreads * kVSide) {
+      const int v0 = b + tid * kVSide;
+      double w[kVSide];
+      weigh<TYPE, kVSide>(f, v0, hi, plain, w);
+      if (finding) {
+        const int found = past_goal<kVSide>(w, v0, goal, &before, &last, s_red, &s_found);
+        if (found == 0x7fffffff) continue;
+        if (tid == 0) a.token[r] = found;
+        return;
+      }
 #pragma unroll
-    for (int i = 0; i < VE; ++i) mine += w[i];
-  }
-  const double sum = group_sum<kVWaves>(mine, s_red);
-  if (p.cuts > 1) {
-    if (tid == 0) {
-      __hip_atomic_store(&p.left[(int64_t)r * p.cuts + cut], sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      s_last = __hip_atomic_fetch_add(&p.tickets[r], 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == p.cuts - 1;
+      for (int i = 0; i < kVSide; ++i) mine += w[i];
     }
-    __syncthreads();
-    if (!s_last) return;
-    if (tid < p.cuts) s_all[tid] = __hip_atomic_load(&p.left[(int64_t)r * p.cuts + tid], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  } else if (tid == 0) {
-    s_all[0] = sum;
+    if (finding) {
+      const int found = last_of(last, &s_found);
+      if (tid == 0) a.token[r] = found;
+      return;
+    }
+    mine = group_sum<kVWaves>(mine, s_red);
+    if (!plain) {
+      if (tid == 0) {
+        // The sums are written and read past the caches (agent scope), so that the ticket
+        // only has to wait for its own: no cache is written back or emptied for it.
+        __hip_atomic_store(&d.left[(int64_t)r * d.cuts + cut], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        s_last = __hip_atomic_fetch_add(&d.tickets[r], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == d.cuts - 1;
+      }
+      __syncthreads();
+      if (!s_last) return;
+      mine = lane < d.cuts ? __hip_atomic_load(&d.left[(int64_t)r * d.cuts + lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+    } else {
+      if (tid == 0) s_all[x] = mine;
+      if (++x < d.cuts) {
+        cut_of(d, x, &lo, &hi);
+        continue;
+      }
+      __syncthreads();
+      mine = lane < d.cuts ? s_all[lane] : 0.0;
+    }
+    const double total = wave_sum(mine);
+    if (!plain && !(total > 0)) {
+      plain = true;
+      cut_of(d, 0, &lo, &hi);
+      continue;
+    }
+    goal = goal_of(a, r, total);
+    // the cut: the first with which the sum is past the goal, or the last that has any
+    double run = mine;
+#pragma unroll
+    for (int y = 1; y < 64; y <<= 1) {
+      const double up = __shfl_up(run, y, 64);
+      if (lane >= y) run += up;
+    }
+    uint64_t some = __ballot(mine > 0 && run > goal);
+    if (some == 0) {
+      goal = __builtin_huge_val();
+      some = 1ull << (63 - __builtin_clzll(__ballot(mine > 0) | 1));
+    }
+    const int at = __builtin_ctzll(some);
+    before = __shfl(run - mine, at, 64);
+    cut_of(d, at, &lo, &hi);
+    finding = true;
+  }
+}
+
+// All of a request over a small vocabulary, but for its place among the rows: a wave a
+// node's sums, then the walk and the draw.
+template <int TYPE, bool GREEDY>
+__global__ __launch_bounds__(kVThreads) void k_lm_verify_small(VerifyDev d) {
+  typedef typename Elem<TYPE>::Raw Raw;
+  const mca_verify_drafts_args& a = d.a;
+  const bool drawn = a.draft != nullptr && !GREEDY;
+  __shared__ Nodes s;
+  __shared__ int s_found, s_gone[MCA_MAX_NODES];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.x, V = (int)a.n_vocab;
+  int first, n;
+  if (!nodes_of(a, r, &first, &n)) {
+    if (tid == 0) no_walk(a, r);
+    return;
+  }
+  load_nodes<GREEDY>(a, first, n, s);
+  // (also of draft rows that no child was drawn from: nothing looks at them)
+  for (int x = wave; x < n * (drawn ? 2 : 1); x += kVWaves) {
+    const int which = x >= n, i = x - which * n;
+    const Raw* row = (const Raw*)(which ? a.draft : a.target) + (int64_t)(first + i) * (which ? a.draft_row : a.target_row);
+    float z[kVSmall / 64], m = GREEDY ? -__builtin_huge_valf() : kLowest, sum = 0.f;
+    int at = V;
+#pragma unroll
+    for (int j = 0; j < kVSmall / 64; ++j) {
+      z[j] = -__builtin_huge_valf();
+      if (64 * j < V && lane + 64 * j < V) z[j] = to_f32<TYPE>(row[lane + 64 * j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kVSmall / 64; ++j) {
+      if (z[j] > m) {
+        m = z[j];
+        at = lane + 64 * j;
+      }
+      if constexpr (GREEDY) sum += z[j] < __builtin_huge_valf() ? 0.f : __builtin_nanf("");
+    }
+#pragma unroll
+    for (int y = 1; y < 64; y <<= 1) {
+      const float m2 = __shfl_xor(m, y, 64);
+      if constexpr (GREEDY) {
+        const int at2 = __shfl_xor(at, y, 64);
+        if (m2 > m || (m2 == m && at2 < at)) at = at2;
+      }
+      m = fmaxf(m, m2);
+    }
+    if constexpr (!GREEDY) {
+      const float k2 = (float)((which ? a.draft_scale : a.scale) * 1.4426950408889634);
+#pragma unroll
+      for (int j = 0; j < kVSmall / 64; ++j)
+        if (64 * j < V) sum += __builtin_amdgcn_exp2f((z[j] - m) * k2);
+    }
+    double total = wave_sum((double)sum);
+    if constexpr (GREEDY) total = total == 0 && at < V ? 1.0 : 0.0;
+    if (lane == 0) {
+      s.m[which][i] = m;
+      s.sum[which][i] = total > 0 ? total : 0.0;  // NaN: none
+      if (which == 0) s.best[i] = at;
+    }
   }
   __syncthreads();
-  double total = 0;
-  for (int x = 0; x < p.cuts; ++x) total += s_all[x];
+  const End e = walk<TYPE, GREEDY, kVThreads>(d, r, first, n, s);
+  if (GREEDY || e.row < 0) return;
+  double sp = 1, sq = 1;
+  if (e.c != 0) exp_sums<TYPE, 1>(weights_of<TYPE>(a, e, 1, 1, nullptr, 0), 0, V, s.red, &sp, &sq);
+  const Weights f = weights_of<TYPE>(a, e, sp, sq, s_gone, gone_symbols(a, e, s_gone, &s_found));
+  double total = weight_sum<TYPE, 1>(f, 0, V, false, s.red);
   const bool plain = !(total > 0);  // nothing is left: from p itself
-  if (plain) {
-    for (int x = 0; x < p.cuts; ++x) {
-      int l, h;
-      cut_of(p, x, &l, &h);
-      double m2 = 0;
-      for (int v = l + tid * VE; v < h; v += kVThreads * VE) {
-        double w[VE];
-        weights(v, h, true, w);
-#pragma unroll
-        for (int i = 0; i < VE; ++i) m2 += w[i];
-      }
-      m2 = group_sum<kVWaves>(m2, s_red);
-      if (tid == 0) s_all[x] = m2;
-    }
-    __syncthreads();
-    total = 0;
-    for (int x = 0; x < p.cuts; ++x) total += s_all[x];
+  if (plain) total = weight_sum<TYPE, 1>(f, 0, V, true, s.red);
+  const double goal = goal_of(a, r, total);
+  double before = 0;
+  int last = -1, found = 0x7fffffff;
+#pragma unroll 1
+  for (int b = 0; b < V && found == 0x7fffffff; b += kVThreads) {
+    double w[1];
+    weigh<TYPE, 1>(f, b + tid, V, plain, w);
+    found = past_goal<1>(w, b + tid, goal, &before, &last, s.red, &s_found);
   }
-  const float u = a.sample[r];
-  const double goal = (u >= 0.f ? (double)fminf(u, 0x1.fffffep-1f) : 0.0) * total;
-  // the cut: the first behind which the sum is past the goal, or the last that has any
-  int at = -1, some = 0;
-  double before = 0, run = 0;
-  for (int x = 0; x < p.cuts; ++x) {
-    const double next = run + s_all[x];
-    if (next > goal && at < 0) {
-      at = x;
-      before = run;
-    }
-    if (s_all[x] > 0) some = x;
-    run = next;
-  }
-  const bool rounded = at < 0;  // by the order of the sums alone
-  if (rounded) at = some;
-  cut_of(p, at, &lo, &hi);
-  // a thread's symbols lie side by side
-  const int each = ((hi - lo + kVThreads - 1) / kVThreads + VE - 1) / VE * VE, v0 = lo + tid * each, v1 = min(hi, v0 + each);
-  mine = 0;
-  for (int v = v0; v < v1; v += VE) {
-    double w[VE];
-    weights(v, v1, plain, w);
-#pragma unroll
-    for (int i = 0; i < VE; ++i) mine += w[i];
-  }
-  s_scan[tid] = mine;
-  if (tid == 0) s_found = 0x7fffffff;
-  __syncthreads();
-  for (int x = 0; x < tid; ++x) before += s_scan[x];
-  int last = -1;  // the thread's last symbol that has any
-  if (mine > 0) {
-    bool done = false;
-    for (int v = v0; v < v1 && !done; v += VE) {
-      double w[VE];
-      weights(v, v1, plain, w);
-#pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        before += w[i];
-        if (w[i] > 0) last = v + i;
-        if (!done && !rounded && w[i] > 0 && before > goal) {
-          atomicMin(&s_found, v + i);
-          done = true;
-        }
-      }
-    }
-  }
-  __syncthreads();
-  if (s_found == 0x7fffffff) {
-    // the sums' rounding leaves none: the last symbol that has any
-    __syncthreads();
-    if (tid == 0) s_found = -1;
-    __syncthreads();
-    atomicMax(&s_found, last);
-    __syncthreads();
-  }
-  if (tid == 0) a.token[r] = s_found;
+  if (found == 0x7fffffff) found = last_of(last, &s_found);
+  if (tid == 0) a.token[r] = found;
 }
 
 namespace {
@@ -606,7 +861,8 @@ int row_splits(const mca_verify_drafts_args& a) {
 }
 int end_cuts(const mca_verify_drafts_args& a) {
   const int64_t reqs = std::max(1, a.n_req);
-  return (int)std::clamp<int64_t>(std::min((1024 + reqs - 1) / reqs, a.n_vocab / 2048), 1, kVMaxSplits);
+  const int64_t cuts = (a.n_vocab + kVCut - 1) / kVCut;
+  return (int)std::clamp<int64_t>(std::min(cuts, std::max((4096 + reqs - 1) / reqs, (cuts + 3) / 4)), 1, kVMaxSplits);
 }
 size_t room(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -643,14 +899,22 @@ void launch(const VerifyDev& d, hipStream_t s) {
     hipLaunchKernelGGL(k_lm_verify_compact, dim3(1), threads, 0, s, d);
     return;
   }
+  if (a.n_vocab <= kVSmall) {
+    if (a.greedy)
+      hipLaunchKernelGGL((k_lm_verify_small<TYPE, true>), dim3((unsigned)a.n_req), threads, 0, s, d);
+    else
+      hipLaunchKernelGGL((k_lm_verify_small<TYPE, false>), dim3((unsigned)a.n_req), threads, 0, s, d);
+    hipLaunchKernelGGL(k_lm_verify_compact, dim3(1), threads, 0, s, d);
+    return;
+  }
   if (a.greedy) {
     if (a.n_rows > 0) hipLaunchKernelGGL((k_lm_verify_rows<TYPE, true>), rows, threads, 0, s, d);
-    hipLaunchKernelGGL((k_lm_verify_walk<TYPE, true>), dim3((unsigned)a.n_req), threads, 0, s, d);
+    hipLaunchKernelGGL((k_lm_verify_walk<TYPE, true>), dim3((unsigned)a.n_req), dim3(kWalkThreads), 0, s, d);
     hipLaunchKernelGGL(k_lm_verify_compact, dim3(1), threads, 0, s, d);
     return;
   }
   if (a.n_rows > 0) hipLaunchKernelGGL((k_lm_verify_rows<TYPE, false>), rows, threads, 0, s, d);
-  hipLaunchKernelGGL((k_lm_verify_walk<TYPE, false>), dim3((unsigned)a.n_req), threads, 0, s, d);
+  hipLaunchKernelGGL((k_lm_verify_walk<TYPE, false>), dim3((unsigned)a.n_req), dim3(kWalkThreads), 0, s, d);
   if (both == 2) hipLaunchKernelGGL((k_lm_verify_sums<TYPE>), dim3((unsigned)a.n_req, (unsigned)d.cuts), threads, 0, s, d);
   hipLaunchKernelGGL((k_lm_verify_draw<TYPE>), dim3((unsigned)a.n_req + 1, (unsigned)d.cuts), threads, 0, s, d);
 }

@@ -243,9 +243,10 @@ def _probabilities(z):
 
 
 def verify_drafts(target, draft, tokens, parents, offsets, lengths, accept, sample, scale, draft_scale, greedy, n_rows):
-    """(new_len, rows, token), and the least distance of a decision from its border, as a share of the sum drawn from."""
+    """(new_len, rows, token), and the least distances of a child's acceptance and of a draw from their borders, as shares
+    of the sum drawn from."""
     V = target.shape[1]
-    new_len, rows, out, margin = [], [], [], 1.0
+    new_len, rows, out, margin, drawn = [], [], [], 1.0, 1.0
     for r in range(len(lengths)):
         a, b = int(offsets[r]), int(offsets[r + 1])
         if a < 0 or b <= a or b > n_rows:
@@ -287,7 +288,7 @@ def verify_drafts(target, draft, tokens, parents, offsets, lengths, accept, samp
                         left = p
                     ends = np.cumsum(left)
                     u = min(max(float(sample[r]), 0.0), 1 - 2.0 ** -24) * ends[-1]
-                    margin = min(margin, np.abs(ends[:-1] - u).min(initial=ends[-1]) / ends[-1])
+                    drawn = min(drawn, np.abs(ends[:-1] - u).min(initial=ends[-1]) / ends[-1])
                     over = np.nonzero(ends > u)[0]
                     token = int(over[0]) if len(over) else int(np.nonzero(left)[0][-1])
             if go is None:
@@ -297,7 +298,7 @@ def verify_drafts(target, draft, tokens, parents, offsets, lengths, accept, samp
         new_len.append(int(lengths[r]) + len(path))
         rows += path
         out.append(token)
-    return np.array(new_len), np.array(rows + [-1] * (n_rows - len(rows))), np.array(out), margin
+    return np.array(new_len), np.array(rows + [-1] * (n_rows - len(rows))), np.array(out), margin, drawn
 
 
 def distill(z, logprob, ids, scale, rest):

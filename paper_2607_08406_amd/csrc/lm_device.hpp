@@ -103,4 +103,44 @@ __device__ __forceinline__ void unpack(u32x4 x, float (&f)[Elem<TYPE>::kPer]) {
   }
 }
 
+// Exponentials and logarithms of 64 bits (the library's are made for all numbers).
+// exp(x) of N numbers of at most 700, to 2^-47: 2^n times the series of exp in the rest,
+// which is at most ln 2 / 2, to its 11th power.  Results below 2^-1021 are 0, NaN stays.
+// The steps of several go side by side: one by one, each would wait for the one before.
+template <int N>
+__device__ __forceinline__ void exps_of(double (&x)[N]) {
+  constexpr double kInvLn2 = 1.4426950408889634074, kLn2 = 0.69314718055994530942, kLn2Rest = 2.3190468138462996e-17;
+  constexpr double kOver[12] = {1.0,          1.0,           1.0 / 2,        1.0 / 6,         1.0 / 24,         1.0 / 120,
+                                1.0 / 720,    1.0 / 5040,    1.0 / 40320,    1.0 / 362880,    1.0 / 3628800,    1.0 / 39916800};  // 1 / k!
+  double n[N], r[N], y[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) n[i] = __builtin_rint(x[i] * kInvLn2);
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = fma(n[i], -kLn2, x[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) r[i] = fma(n[i], -kLn2Rest, r[i]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) y[i] = kOver[11];
+#pragma unroll
+  for (int k = 10; k >= 0; --k) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) y[i] = fma(y[i], r[i], kOver[k]);
+    if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = x[i] < -708.0 ? 0.0 : __builtin_ldexp(y[i], (int)n[i]);
+}
+__device__ __forceinline__ double exp_of(double x) {
+  double y[1] = {x};
+  exps_of(y);
+  return y[0];
+}
+// log(x) of a number that is normal in 32 bits, to 2^-45: its 32-bit logarithm l and the
+// logarithm of x exp(-l), which is next to 1.
+__device__ __forceinline__ double log_of(double x) {
+  const double l = 0.69314718055994530942 * (double)__builtin_amdgcn_logf((float)x);
+  const double y = fma(x, exp_of(-l), -1.0);
+  return l + y * fma(y, -0.5, 1.0);
+}
+
 }  // namespace mca

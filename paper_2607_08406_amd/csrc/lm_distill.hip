@@ -61,167 +61,219 @@ __device__ __forceinline__ double wave_sum(double x) {
   for (int d = 1; d < 64; d <<= 1) x += __shfl_xor(x, d, 64);
   return x;
 }
-// The teacher's probabilities of the wave's entries, and of all other symbols.
-struct Teacher {
-  double q, rest, total;
-  bool any;
+// A number of lane `from`, in all lanes.
+__device__ __forceinline__ double lane_of(double x, int from) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)b, from), hi = __builtin_amdgcn_readlane((uint32_t)(b >> 32), from);
+  return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+// Logarithms of the teacher's probabilities, relative to the largest without rest: no
+// entry has any if that is -inf (`none`).
+struct Logs {
+  double x;
+  bool any, none;
 };
 template <class Args>
-__device__ __forceinline__ Teacher teacher_of(const Args& p, const Entry& e) {
-  Teacher r;
+__device__ __forceinline__ Logs logs_of(const Args& p, const Entry& e) {
+  const float lp = e.id >= 0 ? e.logprob : -__builtin_huge_valf();
+  Logs r;
   r.any = __ballot(e.id >= 0) != 0;
-  double t = e.id >= 0 ? (double)e.logprob * (double)p.scale : -__builtin_huge_val();
+  r.none = false;
+  r.x = (double)lp;
   if (p.rest == 0) {
-    double top = t;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top = fmax(top, __shfl_xor(top, d, 64));
-    const bool none = top == -__builtin_huge_val() && __ballot(t != t) == 0;
-    r.q = none ? 0.0 : exp(t - top);
-    const double sum = wave_sum(r.q);
-    r.q = none ? 0.0 : r.q / sum;
-    r.rest = 0;
-    r.total = wave_sum(r.q);
-  } else {
-    r.q = exp(t);
-    const double sum = wave_sum(r.q);
-    r.rest = r.any ? fmax(1.0 - sum, 0.0) : 0.0;
-    r.total = sum + r.rest;
-    if (!(sum < __builtin_huge_val())) r.q = r.total = __builtin_nan("");
+    float top = lp;
+    for (int d = 1; d < p.n_top; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    top = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(top)));
+    r.none = top == -__builtin_huge_valf() && __ballot(lp != lp) == 0;
+    r.x = r.none ? -__builtin_huge_val() : (double)p.scale * ((double)lp - (double)top);
   }
   return r;
 }
+// exp of a number that is at most 700 if it counts: what passes that (a logprob that is no
+// logarithm of a probability) becomes NaN, as +inf does
+__device__ __forceinline__ double prob_of(double x) { return x > 700.0 ? __builtin_nan("") : exp_of(x); }
 
-// The loss of row t from its sums (one wave).
+// What the loss needs of a row's entries (one wave, entry j in lane j): with q_j
+// their probabilities under the teacher, z_j their logits and m the largest of those
+//   loss = part + q (la + k (top - m)) + other (log other - log s_r),
+// part = sum q_j (log q_j - k (z_j - m)), q = sum q_j, for a sum over all symbols of
+// exp(la + k top); with `rest`, s is that of exp(k (z - m)) over the entries' symbols.
+struct Known {
+  double part, q, other, s, norm;  // (without rest, log norm is still to be taken off part)
+  float m;
+  bool any;
+};
 template <int TYPE>
-__device__ __forceinline__ void finish(const mca_distill_args& p, int64_t t, const Entry& e, float m, double s) {
-  const int lane = threadIdx.x & 63;
-  const double k = p.scale, inf = __builtin_huge_val();
-  const typename Elem<TYPE>::Raw* row = (const typename Elem<TYPE>::Raw*)p.logits + t * p.logits_row;
-  const Teacher q = teacher_of(p, e);
-  const double z = e.id >= 0 ? (double)to_f32<TYPE>(row[e.id]) : -inf;
-  // the sum over all symbols, relative to the largest of all
-  double top = m, all = s;
+__device__ __forceinline__ Known known_of(const mca_distill_args& p, int64_t t, const Entry& e) {
+  const int lane = threadIdx.x & 63, K = p.n_top;
+  const double k = p.scale;
+  const float z = e.id >= 0 ? to_f32<TYPE>(((const typename Elem<TYPE>::Raw*)p.logits)[t * p.logits_row + e.id]) : -__builtin_huge_valf();
+  const Logs lp = logs_of(p, e);
+  Known r;
+  r.any = lp.any;
+  float m = z;
+  for (int d = 1; d < K; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
+  m = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(m)));
+  r.m = m;
+  const double y = k * ((double)z - (double)(m == -__builtin_huge_valf() ? 0.f : m));
+  // The entries' probabilities in lanes 0 to 31, in lanes 32 on their exponentials under the
+  // student: one stream of instructions for both.
+  double x = lp.x;
   if (p.rest != 0) {
     bool first = e.id >= 0;  // a symbol counts once
-    for (int j = 0; j < p.n_top; ++j) {
-      const int id = __shfl(e.id, j, 64);
+    for (int j = 0; j < K; ++j) {
+      const int id = __builtin_amdgcn_readlane(e.id, j);
       if (j < lane && id == e.id) first = false;
     }
-    if (z > top) top = z;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) top = fmax(top, __shfl_xor(top, d, 64));
-    all = s * exp(k * ((double)m - top)) + wave_sum(first ? exp(k * (z - top)) : 0.0);
+    const double mine = first ? y : -__builtin_huge_val(), other = __shfl(mine, lane & 31, 64);
+    x = lane < 32 ? x : other;
   }
-  // logarithms beside k times the largest, which cancels from the loss
-  const double la = all == 0 ? -inf : log(all), ls = s == 0 ? -inf : log(s);
-  double part = 0;
-  if (q.q != q.q)
-    part = q.q;
-  else if (q.q > 0)
-    part = z == -inf ? inf : q.q * (log(q.q) - (k * (z - top) - la));
-  double loss = wave_sum(part);
-  if (q.rest > 0) loss += s == 0 ? inf : q.rest * (log(q.rest) - (k * ((double)m - top) + ls - la));
+  double sum = prob_of(x);
+  double part = lane < 32 && (sum > 0 || sum != sum) ? sum * (x - y) : 0.0;
+  if (p.rest == 0 && lane >= 32) sum = 0;
+  for (int d = 1; d < K; d <<= 1) {
+    sum += __shfl_xor(sum, d, 64);
+    part += __shfl_xor(part, d, 64);
+  }
+  const double q = lane_of(sum, 0);
+  part = lane_of(part, 0);
+  r.s = lane_of(sum, 32);
+  r.norm = 1;
+  if (p.rest != 0) {
+    r.q = q;
+    r.other = fmax(1.0 - q, 0.0);
+    r.part = part;
+  } else {
+    r.q = lp.none ? 0.0 : (q != q ? q : 1.0);
+    r.other = 0;
+    r.norm = lp.none ? 1.0 : q;
+    r.part = lp.none ? 0.0 : part / q;
+  }
+  return r;
+}
+// The loss of row t from the pass's sum s relative to m, in lane 0.
+__device__ __forceinline__ void finish(const mca_distill_args& p, int64_t t, const Known& e, float m, double s) {
+  const int lane = threadIdx.x & 63;
+  const double k = p.scale, inf = __builtin_huge_val();
+  const bool rest = p.rest != 0;
+  const double top = rest ? fmax((double)m, (double)e.m) : (double)m;
+  double all = s;
+  if (rest) {
+    // exponentials of both maxima, a lane each
+    const double f = exp_of(k * ((double)(lane == 0 ? m : e.m) - top));
+    all = s * lane_of(f, 0) + (e.s == 0 ? 0.0 : e.s * lane_of(f, 1));
+  }
+  // logarithms beside k times the largest, which cancels from the loss; of three numbers
+  // in a lane each
+  const double l = log_of(lane == 0 ? all : (lane == 1 ? (rest ? s : e.norm) : (e.other > 0x1p-100 ? e.other : 1.0)));
+  const double la = all == 0 ? -inf : lane_of(l, 0), ls = s == 0 ? -inf : lane_of(l, 1);
+  const double part = rest ? e.part : e.part - lane_of(l, 1);
+  double loss = 0;
+  if (e.q != e.q)
+    loss = e.q;
+  else if (part == inf)
+    loss = inf;
+  else if (!(e.q == 0))
+    loss = part + e.q * (la + k * (top - (e.m == -__builtin_huge_valf() ? 0.0 : (double)e.m)));
+  if (e.other > 0) loss += s == 0 ? inf : e.other * (lane_of(l, 2) - (k * ((double)m - top) + ls - la));
   if (all != all) loss = all;
   if (lane == 0) {
-    p.loss[t] = q.any ? (float)loss : 0.f;
+    p.loss[t] = e.any ? (float)loss : 0.f;
     p.lse[t] = (float)(all == 0 ? -inf : k * top + la);
-    if (p.rest != 0) p.lse_rest[t] = (float)(s == 0 ? -inf : k * (double)m + ls);
+    if (rest) p.lse_rest[t] = (float)(s == 0 ? -inf : k * (double)m + ls);
   }
 }
-
-// Which of a part's vectors hold a symbol of the teacher's: bits in LDS.
-constexpr int kFlagWords = 1024;  // of up to 32768 vectors at a time
 
 }  // namespace
 
 // Rows of more than kDsSmall symbols: a workgroup per row, or per part of one (grid y),
-// in one pass.
+// in one pass of its first four waves; the fifth has the row's entries meanwhile.
 template <int TYPE>
-__global__ __launch_bounds__(kDsThreads) void k_lm_distill(mca_distill_args p, int splits, Sums* parts) {
+__global__ __launch_bounds__(kDsThreads + 64) void k_lm_distill(mca_distill_args p, int splits, Sums* parts) {
   constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
   typedef typename Elem<TYPE>::Raw Raw;
-  __shared__ uint32_t s_flag[kFlagWords];
-  __shared__ int s_id[MCA_MAX_TOP];
   __shared__ Sums s_sums[kDsWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t t = blockIdx.x;
-  const int split = blockIdx.y, V = (int)p.n_vocab, K = p.n_top;
+  const int split = blockIdx.y, V = (int)p.n_vocab;
   const float k2 = p.scale * kLog2e;
   const Raw* row = (const Raw*)p.logits + t * p.logits_row;
   const int head = (int)(((16 - ((uintptr_t)row & 15)) & 15) / EL);
   const int nvec = (V - head) / VE, tail = V - head - nvec * VE;
   const u32x4* vec = (const u32x4*)(row + head);
   const int per = (nvec + splits - 1) / splits, v0 = min(split * per, nvec), v1 = min(nvec, v0 + per);
-  const Entry e = entry_of(p, t, lane);  // every wave has them
-  const bool rest = p.rest != 0;
-  if (wave == 0 && lane < K) s_id[lane] = e.id;
-  Sums a = {kLowest, 0.f};
-  // the values of symbols first .. first + VE - 1; `known`: some may be the teacher's
-  auto take = [&](float (&f)[VE], int first, bool known) {
-    if (known)
-      for (int j = 0; j < K; ++j) {
-        const int at = s_id[j] - first;
-        if (s_id[j] < 0 || at < 0 || at >= VE) continue;
+  const Entry e = entry_of(p, t, lane);       // every wave has them
+  const int mine = p.rest != 0 ? e.id : -1;  // to be left out
+  if (wave == kDsWaves) {
+    Known known{};
+    if (splits == 1) known = known_of<TYPE>(p, t, e);
+    __syncthreads();
+    Sums a = s_sums[0];
 #pragma unroll
-        for (int i = 0; i < VE; ++i) f[i] = i == at ? -__builtin_huge_valf() : f[i];
-      }
-    float cm = f[0];
-#pragma unroll
-    for (int i = 1; i < VE; ++i) cm = fmaxf(cm, f[i]);
-    if (cm > a.m) a.move(cm, k2);
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < VE; ++i) sum += __builtin_amdgcn_exp2f((f[i] - a.m) * k2);
-    a.s += sum;
-  };
-  auto take_some = [&](int v, int n) {
-    float f[VE];
-#pragma unroll
-    for (int i = 0; i < VE; ++i) f[i] = i < n ? to_f32<TYPE>(row[v + i]) : -__builtin_huge_valf();
-    take(f, v, rest);
-  };
-  __syncthreads();
-  if (head > 0 && split == 0 && tid == 0) take_some(0, head);
-  for (int c0 = v0; c0 < v1; c0 += 32 * kFlagWords) {
-    const int c1 = min(v1, c0 + 32 * kFlagWords);
-    if (rest) {
-      __syncthreads();
-      for (int i = tid; i < (c1 - c0 + 31) / 32; i += kDsThreads) s_flag[i] = 0;
-      __syncthreads();
-      if (wave == 0 && e.id >= head) {
-        const int v = (e.id - head) / VE;
-        if (v >= c0 && v < c1) atomicOr(&s_flag[(v - c0) >> 5], 1u << ((v - c0) & 31));
-      }
-      __syncthreads();
-    }
-    for (int b = c0 + wave * 64 * kDsUnroll; b < c1; b += kDsWaves * 64 * kDsUnroll) {
-      u32x4 x[kDsUnroll];
-#pragma unroll
-      for (int u = 0; u < kDsUnroll; ++u) x[u] = gload(vec + min(b + 64 * u + lane, c1 - 1));
-#pragma unroll
-      for (int u = 0; u < kDsUnroll; ++u) {
-        const int v = b + 64 * u + lane;
-        if (v >= c1) continue;
-        const bool known = rest && ((s_flag[(v - c0) >> 5] >> ((v - c0) & 31)) & 1);
-        float f[VE];
-        unpack<TYPE>(x[u], f);
-        take(f, head + v * VE, known);
-      }
-    }
+    for (int w = 1; w < kDsWaves; ++w) a.join(s_sums[w].m, s_sums[w].s, k2);
+    if (splits == 1)
+      finish(p, t, known, a.m, a.s);
+    else if (lane == 0)
+      parts[t * splits + split] = a;
+    return;
   }
-  if (tail > 0 && split == splits - 1 && tid == kDsThreads - 1) take_some(V - tail, tail);
+  Sums a = {kLowest, 0.f};
+  // `n` values from v on, of one lane
+  auto take_some = [&](int v, int n) {
+    for (int i = 0; i < n; ++i) {
+      const bool out = __ballot(mine == v + i) != 0;
+      const float z = to_f32<TYPE>(row[v + i]);
+      if (lane == 0 && !out) a.join(z < kLowest ? kLowest : z, __builtin_amdgcn_exp2f((z - (z < kLowest ? kLowest : z)) * k2), k2);
+    }
+  };
+  for (int b = v0 + wave * 64 * kDsUnroll; b < v1; b += kDsWaves * 64 * kDsUnroll) {
+    u32x4 x[kDsUnroll];
+#pragma unroll
+    for (int u = 0; u < kDsUnroll; ++u) x[u] = gload(vec + min(b + 64 * u + lane, v1 - 1));
+    // the teacher's symbols among these: their values become -inf
+    const int s0 = head + b * VE;
+    for (uint64_t some = __ballot(mine >= s0 && mine - s0 < 64 * kDsUnroll * VE); some != 0; some &= some - 1) {
+      const int in = __builtin_amdgcn_readlane(mine, (int)__builtin_ctzll(some)) - s0, v = in / VE, word = in % VE * EL / 4;
+      const uint32_t low = TYPE == MCA_TYPE_F32 ? 0xff800000u : (TYPE == MCA_TYPE_BF16 ? 0xff80u : 0xfc00u);
+      const int shift = EL == 4 ? 0 : 16 * (in & 1);
+      const uint32_t keep = EL == 4 ? 0u : 0xffff0000u >> shift;
+#pragma unroll
+      for (int u = 0; u < kDsUnroll; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool this_one = v == 64 * u + lane && i == word;
+          x[u][i] = this_one ? (x[u][i] & keep) | (low << shift) : x[u][i];
+        }
+    }
+    float top = -__builtin_huge_valf();
+#pragma unroll
+    for (int u = 0; u < kDsUnroll; ++u) {
+      float f[VE];
+      unpack<TYPE>(x[u], f);
+#pragma unroll
+      for (int i = 0; i < VE; ++i) top = fmaxf(top, f[i]);
+    }
+    // (vectors behind the last are read twice: they do not raise the maximum)
+    if (top > a.m) a.move(top, k2);
+    float sum[kDsUnroll];
+#pragma unroll
+    for (int u = 0; u < kDsUnroll; ++u) {
+      float f[VE];
+      unpack<TYPE>(x[u], f);
+      sum[u] = 0.f;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) sum[u] += __builtin_amdgcn_exp2f((f[i] - a.m) * k2);
+      sum[u] = b + 64 * u + lane < v1 ? sum[u] : 0.f;
+    }
+    a.s += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+  }
+  static_assert(kDsUnroll == 4, "sums of a round");
+  if (head > 0 && split == 0 && wave == 0) take_some(0, head);
+  if (tail > 0 && split == splits - 1 && wave == kDsWaves - 1) take_some(V - tail, tail);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) a.join(__shfl_xor(a.m, d, 64), __shfl_xor(a.s, d, 64), k2);
   if (lane == 0) s_sums[wave] = a;
   __syncthreads();
-  if (wave != 0) return;
-  a = s_sums[0];
-#pragma unroll
-  for (int w = 1; w < kDsWaves; ++w) a.join(s_sums[w].m, s_sums[w].s, k2);
-  if (splits == 1)
-    finish<TYPE>(p, t, e, a.m, a.s);
-  else if (lane == 0)
-    parts[t * splits + split] = a;
 }
 
 template <int TYPE>
@@ -233,7 +285,7 @@ __global__ __launch_bounds__(64) void k_lm_distill_join(mca_distill_args p, int 
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
   const double f = exp((double)p.scale * ((double)x.m - (double)m));
-  finish<TYPE>(p, t, entry_of(p, t, lane), m, wave_sum(f * x.s));
+  finish(p, t, known_of<TYPE>(p, t, entry_of(p, t, lane)), m, wave_sum(f * x.s));
 }
 
 // Rows of at most 64 N symbols: a wave per row, the row in registers.
@@ -265,7 +317,7 @@ __global__ __launch_bounds__(kDsThreads) void k_lm_distill_small(mca_distill_arg
   for (int d = 1; d < 64; d <<= 1) m = fmaxf(m, __shfl_xor(m, d, 64));
 #pragma unroll
   for (int i = 0; i < N; ++i) s += __builtin_amdgcn_exp2f((z[i] - m) * k2);
-  finish<TYPE>(p, t, e, m, wave_sum((double)s));
+  finish(p, t, known_of<TYPE>(p, t, e), m, wave_sum((double)s));
 }
 
 namespace {
@@ -276,19 +328,30 @@ struct RowGrad {
   float lse, lse_other, known, other;
   bool zero;
 };
-__device__ __forceinline__ RowGrad row_grad(const mca_distill_grad_args& p, int64_t t, const Teacher& q, double* off) {
+__device__ __forceinline__ RowGrad row_grad(const mca_distill_grad_args& p, int64_t t, const Entry& e, float* off) {
   RowGrad r;
+  const int lane = threadIdx.x & 63;
   const double g = (double)p.grad_loss[t] * (double)p.scale;
+  const bool rest = p.rest != 0;
+  const Logs lp = logs_of(p, e);
   r.lse = r.lse_other = p.lse[t];
-  r.zero = !q.any || r.lse == -__builtin_huge_valf();
-  r.known = r.other = (float)(g * q.total);
-  if (p.rest != 0) {
-    const float lr = p.lse_rest[t];
-    const bool none = lr == -__builtin_huge_valf();  // then the others' exponentials are 0
-    r.lse_other = none ? 0.f : lr;
-    r.other = none ? 0.f : (float)(g * (q.total * exp((double)lr - (double)r.lse) - q.rest));
+  r.zero = !lp.any || r.lse == -__builtin_huge_valf();
+  const float lr = rest ? p.lse_rest[t] : 0.f;
+  const bool nothing = rest && lr == -__builtin_huge_valf();  // then the others' exponentials are 0
+  // the entries' probabilities, and in lane 63 the student's of the others
+  const double q = prob_of(rest && lane == 63 ? (double)(nothing ? 0.f : lr) - (double)r.lse : lp.x);
+  double sum = lane < 32 ? q : 0.0;
+  for (int d = 1; d < p.n_top; d <<= 1) sum += __shfl_xor(sum, d, 64);
+  sum = lane_of(sum, 0);
+  const double left = rest ? fmax(1.0 - sum, 0.0) : 0.0;
+  // (without rest the entries' sum to 1, if any has some)
+  const double total = rest ? (sum != sum ? sum : sum + left) : (lp.none ? 0.0 : (sum != sum ? sum : 1.0));
+  r.known = r.other = (float)(g * total);
+  if (rest) {
+    r.lse_other = nothing ? 0.f : lr;
+    r.other = nothing ? 0.f : (float)(g * (total * lane_of(q, 63) - left));
   }
-  *off = g * q.q;
+  *off = (float)(lp.none ? 0.0 : g * (rest ? q : q / sum));
   return r;
 }
 __device__ __forceinline__ float prob(float z, float scale, float lse) {
@@ -323,11 +386,11 @@ __global__ __launch_bounds__(kDsThreads) void k_lm_distill_grad(mca_distill_grad
   __syncthreads();
   if (tid < 64) {
     const Entry e = entry_of(p, t, lane);
-    double off;
-    const RowGrad r = row_grad(p, t, teacher_of(p, e), &off);
+    float off;
+    const RowGrad r = row_grad(p, t, e, &off);
     if (lane < K) {
       s_id[lane] = e.id;
-      s_off[lane] = (float)off;
+      s_off[lane] = off;
     }
     if (lane == 0) s_row = r;
     if (e.id >= head) {
@@ -395,9 +458,8 @@ __global__ __launch_bounds__(kDsThreads) void k_lm_distill_grad_rows(mca_distill
   const Raw* row = (const Raw*)p.logits + t * p.logits_row;
   Raw* out = (Raw*)p.grad + t * p.grad_row;
   const Entry e = entry_of(p, t, lane);
-  double off64;
-  const RowGrad r = row_grad(p, t, teacher_of(p, e), &off64);
-  const float off = (float)off64;
+  float off;
+  const RowGrad r = row_grad(p, t, e, &off);
   for (int v0 = 0; v0 < V; v0 += 64) {
     const int v = v0 + lane;
     const float z = v < V ? to_f32<TYPE>(row[v]) : 0.f;
@@ -440,7 +502,7 @@ void launch_distill(const mca_distill_args& a, const LogprobsPlan& plan, hipStre
     hipLaunchKernelGGL((k_lm_distill_small<TYPE, 16>), grid, threads, 0, s, a);
   else {
     Sums* parts = (Sums*)a.workspace;
-    hipLaunchKernelGGL((k_lm_distill<TYPE>), dim3((unsigned)a.n_rows, (unsigned)plan.splits), threads, 0, s, a, plan.splits, parts);
+    hipLaunchKernelGGL((k_lm_distill<TYPE>), dim3((unsigned)a.n_rows, (unsigned)plan.splits), dim3(kDsThreads + 64), 0, s, a, plan.splits, parts);
     if (plan.splits > 1)
       hipLaunchKernelGGL((k_lm_distill_join<TYPE>), dim3((unsigned)a.n_rows), dim3(64), 0, s, a, plan.splits, parts);
   }

@@ -59,37 +59,6 @@ struct VerifyDev {
   int32_t* paths;        // [n_rows]
 };
 
-// exp(x) of N numbers x <= 0, to 2^-47: 2^n times the series of exp in the rest, which is
-// at most ln 2 / 2, to its 11th power.  Results below 2^-1022 are 0, NaN stays.
-// The steps of several go side by side: one by one, each would wait for the one before.
-template <int N>
-__device__ __forceinline__ void exps_of(double (&x)[N]) {
-  constexpr double kInvLn2 = 1.4426950408889634074, kLn2 = 0.69314718055994530942, kLn2Rest = 2.3190468138462996e-17;
-  constexpr double kOver[12] = {1.0,          1.0,           1.0 / 2,        1.0 / 6,         1.0 / 24,         1.0 / 120,
-                                1.0 / 720,    1.0 / 5040,    1.0 / 40320,    1.0 / 362880,    1.0 / 3628800,    1.0 / 39916800};  // 1 / k!
-  double n[N], r[N], y[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) n[i] = __builtin_rint(x[i] * kInvLn2);
-#pragma unroll
-  for (int i = 0; i < N; ++i) r[i] = fma(n[i], -kLn2, x[i]);
-#pragma unroll
-  for (int i = 0; i < N; ++i) r[i] = fma(n[i], -kLn2Rest, r[i]);
-#pragma unroll
-  for (int i = 0; i < N; ++i) y[i] = kOver[11];
-#pragma unroll
-  for (int k = 10; k >= 0; --k) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) y[i] = fma(y[i], r[i], kOver[k]);
-    if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);
-  }
-#pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = x[i] < -708.0 ? 0.0 : __builtin_ldexp(y[i], (int)n[i]);
-}
-__device__ __forceinline__ double exp_of(double x) {
-  double y[1] = {x};
-  exps_of(y);
-  return y[0];
-}
 // 16 bytes at any address
 template <int TYPE>
 __device__ __forceinline__ void load_any(const char* p, float (&f)[Elem<TYPE>::kPer]) {

@@ -53,7 +53,7 @@ def test_the_token_behind_the_root_is_the_targets(mode, kids):
             # the random number of the draw matters only by its quantiles: its mean over a grid
             accept = np.concatenate([[0.0], grid[list(us)]])
             for w in grid[::4]:
-                new, path, tok, _ = lm.verify_drafts(rows, dr, np.array([0, *toks]), np.array([-1] + [0] * kids), [0, n], [0], accept,
+                new, path, tok, _, _ = lm.verify_drafts(rows, dr, np.array([0, *toks]), np.array([-1] + [0] * kids), [0, n], [0], accept,
                                                      [w], 1.0, 1.0, False, n)
                 first = toks[path[1] - 1] if new[0] > 1 else tok[0]
                 seen[first] += weight
@@ -64,7 +64,7 @@ def test_greedy_and_paths():
     z = np.zeros((5, 4))
     z[0, 2], z[1, 1], z[3, 3] = 1, 1, 1
     # node 0 has children 1 (token 0), 2 (token 2), 3 (token 2); node 2 has child 4
-    new, rows, tok, _ = lm.verify_drafts(z, None, np.array([9, 0, 2, 2, 0]), np.array([-1, 0, 0, 0, 2]), [0, 5], [7], None, None, 1, 1,
+    new, rows, tok, _, _ = lm.verify_drafts(z, None, np.array([9, 0, 2, 2, 0]), np.array([-1, 0, 0, 0, 2]), [0, 5], [7], None, None, 1, 1,
                                          True, 6)
     assert new[0] == 10 and rows.tolist() == [0, 2, 4, -1, -1, -1] and tok[0] == 0
 

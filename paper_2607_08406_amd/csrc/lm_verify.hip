@@ -29,8 +29,8 @@ constexpr int kVMaxSplits = 64;   // parts of a row
 constexpr int64_t kVPart = 8192;  // symbols of a part at least
 constexpr int kVSide = 8;         // symbols side by side in a thread of the draw
 constexpr int kVCut = 4096;       // symbols of a cut of the draw, but for very large vocabularies
-// Largest vocabulary of the kernel that does all of a request in one workgroup.
-constexpr int kVSmall = 1024;
+constexpr int kVSegment = 256;    // symbols that a wave weighs at a time in the kernel of whole requests
+constexpr int kVWhole = 32 * kVSegment;  // its largest vocabulary (64 segments at most)
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -435,24 +435,12 @@ __device__ __forceinline__ void weigh(const Weights& f, int v, int hi, bool plai
       for (int i = 0; i < E; ++i) w[i] = i == out ? 0.0 : w[i];
     }
 }
-template <int TYPE, int E>
-__device__ __forceinline__ double weight_sum(const Weights& f, int lo, int hi, bool plain, double* s_red) {
-  double mine = 0;
-#pragma unroll 1
-  for (int v = lo + (int)threadIdx.x * E; v < hi; v += kVThreads * E) {
-    double w[E];
-    weigh<TYPE, E>(f, v, hi, plain, w);
-#pragma unroll
-    for (int i = 0; i < E; ++i) mine += w[i];
-  }
-  return group_sum<kVWaves>(mine, s_red);
-}
 // The sums of both softmaxes' exponentials over symbols lo .. hi - 1.
-template <int TYPE, int E>
+template <int TYPE, int E, int THREADS>
 __device__ __forceinline__ void exp_sums(const Weights& f, int lo, int hi, double* s_red, double* sp, double* sq) {
   double sum[2] = {0, 0};
 #pragma unroll 1
-  for (int v = lo + (int)threadIdx.x * E; v < hi; v += kVThreads * E) {
+  for (int v = lo + (int)threadIdx.x * E; v < hi; v += THREADS * E) {
     float x[E], y[E];
     symbols<TYPE, E>(f.zt, v, hi, x);
     symbols<TYPE, E>(f.zd, v, hi, y);
@@ -469,8 +457,8 @@ __device__ __forceinline__ void exp_sums(const Weights& f, int lo, int hi, doubl
       sum[1] += which ? mine : 0.0;
     }
   }
-  *sp = group_sum<kVWaves>(sum[0], s_red);
-  *sq = group_sum<kVWaves>(sum[1], s_red);
+  *sp = group_sum<THREADS / 64>(sum[0], s_red);
+  *sq = group_sum<THREADS / 64>(sum[1], s_red);
 }
 
 __device__ __forceinline__ double goal_of(const mca_verify_drafts_args& a, int r, double total) {
@@ -600,7 +588,7 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_sums(VerifyDev d) {
   int lo, hi;
   cut_of(d, cut, &lo, &hi);
   double sp, sq;
-  exp_sums<TYPE, kVSide>(weights_of<TYPE>(d.a, e, 1, 1, nullptr, 0), lo, hi, s_red, &sp, &sq);
+  exp_sums<TYPE, kVSide, kVThreads>(weights_of<TYPE>(d.a, e, 1, 1, nullptr, 0), lo, hi, s_red, &sp, &sq);
   if (threadIdx.x == 0) {
     d.sums[(int64_t)r * 2 * d.cuts + cut] = sp;
     d.sums[((int64_t)r * 2 + 1) * d.cuts + cut] = sq;
@@ -742,15 +730,17 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_draw(VerifyDev d) {
   }
 }
 
-// All of a request over a small vocabulary, but for its place among the rows: a wave a
-// node's sums, then the walk and the draw.
+// All of a request in one workgroup, but for its place among the rows: a wave a node's
+// sums, the walk, the weights of 256 symbols a wave, and of those in which the goal lies
+// once more.  The sums of few values are of 64 bits from the start.
 template <int TYPE, bool GREEDY>
-__global__ __launch_bounds__(kVThreads) void k_lm_verify_small(VerifyDev d) {
-  typedef typename Elem<TYPE>::Raw Raw;
+__global__ __launch_bounds__(kWalkThreads) void k_lm_verify_whole(VerifyDev d) {
+  constexpr int THREADS = kWalkThreads, WAVES = THREADS / 64, EACH = kVSegment / 64;
   const mca_verify_drafts_args& a = d.a;
   const bool drawn = a.draft != nullptr && !GREEDY;
   __shared__ Nodes s;
-  __shared__ int s_found, s_gone[MCA_MAX_NODES];
+  __shared__ int s_count, s_gone[MCA_MAX_NODES];
+  __shared__ double s_seg[64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r = blockIdx.x, V = (int)a.n_vocab;
   int first, n;
   if (!nodes_of(a, r, &first, &n)) {
@@ -758,25 +748,41 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_small(VerifyDev d) {
     return;
   }
   load_nodes<GREEDY>(a, first, n, s);
+  const int rows = n * (drawn ? 2 : 1);
+  const bool exact = !GREEDY && rows * V <= 1 << 14;
   // (also of draft rows that no child was drawn from: nothing looks at them)
-  for (int x = wave; x < n * (drawn ? 2 : 1); x += kVWaves) {
+  for (int x = wave; x < rows; x += WAVES) {
     const int which = x >= n, i = x - which * n;
-    const Raw* row = (const Raw*)(which ? a.draft : a.target) + (int64_t)(first + i) * (which ? a.draft_row : a.target_row);
-    float z[kVSmall / 64], m = GREEDY ? -__builtin_huge_valf() : kLowest, sum = 0.f;
+    const char* row = (const char*)(which ? a.draft : a.target) +
+                      (int64_t)(first + i) * (which ? a.draft_row : a.target_row) * Elem<TYPE>::kSize;
+    const double k = which ? a.draft_scale : a.scale;
+    const float k2 = (float)(k * 1.4426950408889634);
+    float m = GREEDY ? -__builtin_huge_valf() : kLowest, sum = 0.f;
     int at = V;
+#pragma unroll 4
+    for (int v = lane * EACH; v < V; v += kVSegment) {
+      float z[EACH];
+      symbols<TYPE, EACH>(row, v, V, z);
+      if constexpr (GREEDY) {
 #pragma unroll
-    for (int j = 0; j < kVSmall / 64; ++j) {
-      z[j] = -__builtin_huge_valf();
-      if (64 * j < V && lane + 64 * j < V) z[j] = to_f32<TYPE>(row[lane + 64 * j]);
-    }
+        for (int j = 0; j < EACH; ++j) {
+          sum += z[j] < __builtin_huge_valf() ? 0.f : __builtin_nanf("");
+          if (z[j] > m) {
+            m = z[j];
+            at = v + j;
+          }
+        }
+      } else {
+        float top = m;
 #pragma unroll
-    for (int j = 0; j < kVSmall / 64; ++j) {
-      if (z[j] > m) {
-        m = z[j];
-        at = lane + 64 * j;
+        for (int j = 0; j < EACH; ++j) top = fmaxf(top, z[j]);
+        sum *= __builtin_amdgcn_exp2f((m - top) * k2);
+        m = top;
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) sum += __builtin_amdgcn_exp2f((z[j] - m) * k2);
       }
-      if constexpr (GREEDY) sum += z[j] < __builtin_huge_valf() ? 0.f : __builtin_nanf("");
     }
+    float own = m;
 #pragma unroll
     for (int y = 1; y < 64; y <<= 1) {
       const float m2 = __shfl_xor(m, y, 64);
@@ -786,13 +792,23 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_small(VerifyDev d) {
       }
       m = fmaxf(m, m2);
     }
-    if constexpr (!GREEDY) {
-      const float k2 = (float)((which ? a.draft_scale : a.scale) * 1.4426950408889634);
+    double total = 0;
+    if (exact) {
+#pragma unroll 1
+      for (int v = lane * EACH; v < V; v += kVSegment) {
+        float z[EACH];
+        symbols<TYPE, EACH>(row, v, V, z);
+        double e[EACH];
 #pragma unroll
-      for (int j = 0; j < kVSmall / 64; ++j)
-        if (64 * j < V) sum += __builtin_amdgcn_exp2f((z[j] - m) * k2);
+        for (int j = 0; j < EACH; ++j) e[j] = k * ((double)z[j] - (double)m);
+        exps_of(e);
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) total += e[j];
+      }
+    } else {
+      total = GREEDY ? (double)sum : (double)sum * (double)__builtin_amdgcn_exp2f((own - m) * k2);
     }
-    double total = wave_sum((double)sum);
+    total = wave_sum(total);
     if constexpr (GREEDY) total = total == 0 && at < V ? 1.0 : 0.0;
     if (lane == 0) {
       s.m[which][i] = m;
@@ -801,25 +817,74 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_small(VerifyDev d) {
     }
   }
   __syncthreads();
-  const End e = walk<TYPE, GREEDY, kVThreads>(d, r, first, n, s);
+  const End e = walk<TYPE, GREEDY, THREADS>(d, r, first, n, s);
   if (GREEDY || e.row < 0) return;
-  double sp = 1, sq = 1;
-  if (e.c != 0) exp_sums<TYPE, 1>(weights_of<TYPE>(a, e, 1, 1, nullptr, 0), 0, V, s.red, &sp, &sq);
-  const Weights f = weights_of<TYPE>(a, e, sp, sq, s_gone, gone_symbols(a, e, s_gone, &s_found));
-  double total = weight_sum<TYPE, 1>(f, 0, V, false, s.red);
-  const bool plain = !(total > 0);  // nothing is left: from p itself
-  if (plain) total = weight_sum<TYPE, 1>(f, 0, V, true, s.red);
-  const double goal = goal_of(a, r, total);
-  double before = 0;
-  int last = -1, found = 0x7fffffff;
+  double sp = s.sum[0][e.node], sq = s.sum[1][e.node];
+  if (e.c != 0 && !exact) exp_sums<TYPE, EACH, THREADS>(weights_of<TYPE>(a, e, 1, 1, nullptr, 0), 0, V, s.red, &sp, &sq);
+  const Weights f = weights_of<TYPE>(a, e, sp, sq, s_gone, gone_symbols(a, e, s_gone, &s_count));
+  const int segments = (V + kVSegment - 1) / kVSegment;
 #pragma unroll 1
-  for (int b = 0; b < V && found == 0x7fffffff; b += kVThreads) {
-    double w[1];
-    weigh<TYPE, 1>(f, b + tid, V, plain, w);
-    found = past_goal<1>(w, b + tid, goal, &before, &last, s.red, &s_found);
+  for (int plain = 0; plain < 2; ++plain) {  // 1: nothing is left, from p itself
+#pragma unroll 1
+    for (int x = wave; x < segments; x += WAVES) {
+      double w[EACH];
+      weigh<TYPE, EACH>(f, x * kVSegment + lane * EACH, V, plain, w);
+      double mine = 0;
+#pragma unroll
+      for (int j = 0; j < EACH; ++j) mine += w[j];
+      mine = wave_sum(mine);
+      if (lane == 0) s_seg[x] = mine;
+    }
+    __syncthreads();
+    const double mine = lane < segments ? s_seg[lane] : 0.0;
+    double run = mine;
+#pragma unroll
+    for (int y = 1; y < 64; y <<= 1) {
+      const double up = __shfl_up(run, y, 64);
+      if (lane >= y) run += up;
+    }
+    const double total = __shfl(run, 63, 64);
+    if (!(total > 0) && plain == 0) {
+      __syncthreads();
+      continue;
+    }
+    if (wave != 0) return;
+    double goal = goal_of(a, r, total);
+    uint64_t some = __ballot(mine > 0 && run > goal);
+    if (some == 0) {  // by the sums' rounding alone: the last that has any weight
+      goal = __builtin_huge_val();
+      some = 1ull << (63 - __builtin_clzll(__ballot(mine > 0) | 1));
+    }
+    const int seg = __builtin_ctzll(some);
+    double at = __shfl(run - mine, seg, 64), w[EACH], own = 0;
+    const int v0 = seg * kVSegment + lane * EACH;
+    weigh<TYPE, EACH>(f, v0, V, plain, w);
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) own += w[j];
+    double ends = own;
+#pragma unroll
+    for (int y = 1; y < 64; y <<= 1) {
+      const double up = __shfl_up(ends, y, 64);
+      if (lane >= y) ends += up;
+    }
+    at += ends - own;
+    int hit = 0x7fffffff, last = -1;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      at += w[j];
+      if (w[j] > 0) {
+        last = v0 + j;
+        if (at > goal) hit = min(hit, v0 + j);
+      }
+    }
+#pragma unroll
+    for (int y = 1; y < 64; y <<= 1) {
+      hit = min(hit, __shfl_xor(hit, y, 64));
+      last = max(last, __shfl_xor(last, y, 64));
+    }
+    if (lane == 0) a.token[r] = hit != 0x7fffffff ? hit : last;
+    return;
   }
-  if (found == 0x7fffffff) found = last_of(last, &s_found);
-  if (tid == 0) a.token[r] = found;
 }
 
 namespace {
@@ -831,9 +896,19 @@ int row_splits(const mca_verify_drafts_args& a) {
 int end_cuts(const mca_verify_drafts_args& a) {
   const int64_t reqs = std::max(1, a.n_req);
   const int64_t cuts = (a.n_vocab + kVCut - 1) / kVCut;
-  return (int)std::clamp<int64_t>(std::min(cuts, std::max((4096 + reqs - 1) / reqs, (cuts + 3) / 4)), 1, kVMaxSplits);
+  return (int)std::clamp<int64_t>(std::min(cuts * (reqs * cuts <= 256 ? 2 : 1), std::max((4096 + reqs - 1) / reqs, (cuts + 3) / 4)), 1, kVMaxSplits);
 }
 size_t room(size_t n) { return (n + 255) / 256 * 256; }
+// A request in one workgroup, while its rows are few values in all.  (bf16, 32 requests,
+// us with one workgroup a request and over all of the chip: drafts of 5, 1000 symbols 18 and
+// 25; trees of 8, 2000 symbols 22 and 26, 5000 30 and 31, 16000 72 and 36; 8 requests of 47
+// nodes, 500 symbols 25 and 27; 200 drafts of 4, 6000 symbols 32 and 40; but 4 of one
+// node, 16000 symbols 37 and 27.  Greedy calls need no draw: 64 drafts of 4, 8000 symbols 17
+// and 12.  Four waves instead of 16 are slower: 22 for 18, 46 for 30.)
+bool is_whole(const mca_verify_drafts_args& a) {
+  const int64_t values = a.n_vocab * a.max_nodes * (a.draft != nullptr && !a.greedy ? 2 : 1);
+  return a.n_vocab <= kVWhole && values <= (a.greedy ? 1 << 13 : 1 << 16);
+}
 
 // The workspace's regions; returns its size.
 size_t lay_out(const mca_verify_drafts_args& a, VerifyDev* d) {
@@ -868,11 +943,11 @@ void launch(const VerifyDev& d, hipStream_t s) {
     hipLaunchKernelGGL(k_lm_verify_compact, dim3(1), threads, 0, s, d);
     return;
   }
-  if (a.n_vocab <= kVSmall) {
+  if (is_whole(a)) {
     if (a.greedy)
-      hipLaunchKernelGGL((k_lm_verify_small<TYPE, true>), dim3((unsigned)a.n_req), threads, 0, s, d);
+      hipLaunchKernelGGL((k_lm_verify_whole<TYPE, true>), dim3((unsigned)a.n_req), dim3(kWalkThreads), 0, s, d);
     else
-      hipLaunchKernelGGL((k_lm_verify_small<TYPE, false>), dim3((unsigned)a.n_req), threads, 0, s, d);
+      hipLaunchKernelGGL((k_lm_verify_whole<TYPE, false>), dim3((unsigned)a.n_req), dim3(kWalkThreads), 0, s, d);
     hipLaunchKernelGGL(k_lm_verify_compact, dim3(1), threads, 0, s, d);
     return;
   }

@@ -1,0 +1,204 @@
+"""Drafts, their verification and the caches together, as they serve: mca_extend on drafted
+nodes, mca_verify_drafts on its logits, mca_block_tables on the lengths that it gives
+and mca_cache_append on the rows; and the same step over a cache of 8-bit values
+(mca_tree_attention8, mca_cache8_append), eagerly and captured.  No number leaves the
+GPU between the calls.
+"""
+from dataclasses import replace
+
+import numpy as np
+import pytest
+import torch
+
+from lm8_util import codes, host, put
+from oracle import lm as olm
+from workloads import CONFIGS, transformer_workload
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def lm():
+    from paper_2607_08406_amd import lm as m
+    assert torch.cuda.is_available()
+    return m
+
+
+def make_context():
+    from paper_2607_08406_amd import mca
+    cfg = replace(CONFIGS["transformer"], ctx=48, d_model=64, n_head=2, n_seq=2, d_mlp=96)
+    w = transformer_workload(cfg)
+    rng = np.random.default_rng(5)
+    # weights of a trained net's size, so that its choices hang on the text
+    params = [p if p.ndim == 1 else (p * rng.uniform(1, 6)).astype(np.float32) for p in w["params"]]
+    desc = mca.transformer_desc(cfg.vocab, cfg.ctx, cfg.d_model, cfg.n_layer, cfg.n_head, cfg.d_mlp, delta=cfg.delta,
+                                ln_eps=cfg.ln_eps, seed=cfg.seed_stream, stream_tag=cfg.stream_tag)
+    return mca.TransformerContext(desc, params, w["tokens"], w["targets"], k_max=2), cfg
+
+
+class Pages:
+    """Caches of the net's blocks, tables and lengths on the GPU."""
+
+    def __init__(self, lm, cfg, R, block=4):
+        self.lm, self.cfg, self.R, self.block = lm, cfg, R, block
+        n = R * (-(-cfg.ctx // block)) + 2
+        self.cache = [torch.zeros(cfg.n_layer, n, cfg.n_head, block, 32, device="cuda") for _ in range(2)]
+        self.table = torch.full((R, -(-cfg.ctx // block)), -1, dtype=torch.int32, device="cuda")
+        self.free = torch.randperm(n, device="cuda").int()
+        self.lens = torch.zeros(R, dtype=torch.int32, device="cuda")
+        self.status = torch.zeros(4, dtype=torch.int32, device="cuda")
+
+    def step(self, ctx, tokens, parents, offsets, max_nodes, **verify):
+        """The nodes through the net; those that verify accepts are kept.  Returns the tokens that follow."""
+        logits, qkv = ctx.extend(tokens, parents, offsets, self.lens, self.table, *self.cache, max_nodes, max_len=self.cfg.ctx)
+        got = self.lm.mca_verify_drafts(logits, None, tokens, parents, offsets, self.lens, max_nodes, **verify)
+        n = tokens.numel()
+        slots, first = torch.zeros(n, dtype=torch.int64, device="cuda"), torch.zeros(self.R + 1, dtype=torch.int32, device="cuda")
+        self.lm.mca_block_tables(self.lens, got.new_len, self.table, self.free, self.block, first, slots, self.status)
+        for b in range(self.cfg.n_layer):
+            self.lm.mca_cache_append(qkv[b, :, 1], qkv[b, :, 2], self.cache[0][b], self.cache[1][b], slots, got.rows)
+        self.lens = got.new_len
+        return got.token
+
+
+def test_greedy_drafts_give_the_text_of_single_tokens(lm):
+    """Whatever the drafts are, accepted ones and the tokens behind them are what the net says one at a time."""
+    ctx, cfg = make_context()
+    R, steps = 5, 30
+    rng = np.random.default_rng(3)
+    start = put(rng.integers(0, cfg.vocab, R))
+    single, one = Pages(lm, cfg, R), put(np.arange(R + 1))
+    text, tok = [host(start)], start
+    for _ in range(steps):
+        tok = single.step(ctx, tok, put([-1] * R), one, 1, greedy=True)
+        text.append(host(tok))
+    text = np.array(text).T.astype(int)  # [R, steps + 1]
+    assert (host(single.lens) == steps).all() and (text >= 0).all()
+    pages, tok = Pages(lm, cfg, R), start
+    made, at, accepted = [[int(t)] for t in host(start)], np.zeros(R, int), 0
+    while at.max() + 5 <= steps:
+        # a tree for each request: the right continuation of up to three tokens, mostly, beside wrong ones
+        tokens, parents, counts = [], [], []
+        for r in range(R):
+            nodes, up = [made[r][-1]], [-1]
+            for i in range(int(rng.integers(0, 4))):
+                wrong = int(rng.integers(0, cfg.vocab))
+                nodes += [wrong, int(text[r, at[r] + 1 + i]) if rng.random() < 0.8 else wrong]
+                up += [len(nodes) - 3 if i else 0] * 2
+            tokens += nodes
+            parents += up
+            counts.append(len(nodes))
+        offsets = put(np.concatenate([[0], np.cumsum(counts)]))
+        before = host(pages.lens)
+        tok = pages.step(ctx, put(tokens), put(parents), offsets, max(counts), greedy=True)
+        took = (host(pages.lens) - before).astype(int)
+        accepted += int((took - 1).sum())
+        for r in range(R):
+            at[r] += took[r]
+            made[r] = list(text[r, :at[r]]) + [int(host(tok)[r])]
+            assert made[r][-1] == text[r, at[r]]
+    assert accepted > 5 and int(pages.status[0]) == 0
+    # and the caches hold the same tokens' keys: the net's own, off by the products' order
+    for r in range(R):
+        ids, other = host(pages.table)[r], host(single.table)[r]
+        for t in range(int(at[r])):
+            a = pages.cache[0][:, ids[t // 4], :, t % 4]
+            b = single.cache[0][:, other[t // 4], :, t % 4]
+            assert (a - b).abs().max() <= 8 * 512 * 2.0 ** -24 * b.abs().max().clamp(min=1)
+    ctx.close()
+
+
+@pytest.mark.parametrize("typ", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("captured", [False, True])
+def test_a_step_over_the_cache_of_8_bits(lm, typ, captured):
+    """One attention layer between an embedding and a projection, on drafted trees; every output of every call against
+    the oracle on what the call was given."""
+    R, n, H, G, D, B, V = 6, 7, 2, 2, 64, 8, 90
+    rng = np.random.default_rng(9)
+    torch.manual_seed(4)
+    width = 16
+    blocks = R * width + 1
+    kc, vc = codes(np.full((blocks, H, B, D), 0x7f)), codes(np.full((blocks, H, B, D), 0x7f))
+    ks, vs = torch.full((blocks, H), 200, dtype=torch.uint8, device="cuda"), torch.full((blocks, H), 200, dtype=torch.uint8, device="cuda")
+    table = torch.full((R, width), -1, dtype=torch.int32, device="cuda")
+    free = torch.randperm(blocks, device="cuda").int()
+    lens = torch.zeros(R, dtype=torch.int32, device="cuda")
+    emb = torch.randn(V, (G * H + 2 * H) * D, device="cuda").to(typ)
+    out_w = (torch.randn(G * H * D, V, device="cuda") * 0.3).to(typ)
+    tokens, parents = put([0] * (R * n)), put([0] * (R * n))
+    offsets = put(np.arange(R + 1) * n)
+    draft = torch.zeros(R * n, V, device="cuda", dtype=typ)
+    accept, sample = torch.zeros(R * n, device="cuda"), torch.zeros(R, device="cuda")
+    slots, first = torch.zeros(R * n, dtype=torch.int64, device="cuda"), torch.zeros(R + 1, dtype=torch.int32, device="cuda")
+    status = torch.zeros(4, dtype=torch.int32, device="cuda")
+    room = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    kept = {}
+
+    def step():
+        x = emb[tokens.long()].view(R * n, G * H + 2 * H, D)
+        q, k, v = x.split([G * H, H, H], 1)
+        att, lse = lm.mca_tree_attention8(q, k, v, kc, vc, ks, vs, table, lens, offsets, parents, n, workspace=room)
+        logits = att.view(R * n, -1) @ out_w
+        got = lm.mca_verify_drafts(logits, draft, tokens, parents, offsets, lens, n, accept, sample, scale=0.8, workspace=room)
+        lm.mca_block_tables(lens, got.new_len, table, free, B, first, slots, status)
+        lm.mca_cache8_append(k, v, kc, vc, ks, vs, table, lens, first, got.rows)
+        kept.update(q=q, k=k, v=v, att=att, lse=lse, logits=logits, got=got)
+
+    state = (kc, vc, ks, vs, table, free, lens)
+    graph = None
+    if captured:
+        saved = [t.clone() for t in state]
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        for t, s in zip(state, saved):
+            (t.view(torch.uint8) if t.dtype == torch.float8_e4m3fn else t).copy_(s.view(torch.uint8) if s.dtype == torch.float8_e4m3fn else s)
+    last, total = rng.integers(0, V, R), 0
+    for _ in range(7):
+        # drafts: a tree each, tokens drawn from draft logits that know the target a little
+        draft.copy_(torch.randn(R * n, V, device="cuda"))
+        d = host(draft).astype(np.float64)
+        tok, up = np.zeros((R, n), int), np.full((R, n), -1)
+        for r in range(R):
+            tok[r, 0] = last[r]
+            for i in range(1, n):
+                up[r, i] = (i - 1) // 2
+                p = np.exp(d[r * n + up[r, i]])
+                tok[r, i] = rng.choice(V, p=p / p.sum())
+        tokens.copy_(put(tok.reshape(-1)))
+        parents.copy_(put(up.reshape(-1)))
+        accept.uniform_()
+        accept.mul_(0.2)  # (a target that likes drafts: more is accepted)
+        sample.uniform_()
+        before = {name: host(t) for name, t in zip(("kc", "vc", "ks", "vs", "table", "free", "lens"), state)}
+        if captured:
+            graph.replay()
+        else:
+            step()
+        torch.cuda.synchronize()
+        h = {name: host(t) for name, t in kept.items() if name != "got"}
+        got = [host(t) for t in kept["got"]]
+        want = olm.tree_attention(h["q"], h["k"], h["v"], olm.cache8_values(before["kc"], before["ks"]),
+                                  olm.cache8_values(before["vc"], before["vs"]), before["table"], before["lens"], host(offsets),
+                                  host(parents), D ** -0.5)
+        eps = torch.finfo(typ).eps / 2
+        for (row, head), (o, norm, pv, sv, size, L) in want.items():
+            e32 = 2 * (D + 8) * 2.0 ** -24 * size + (L + 16) * 2.0 ** -24
+            tol = 1.02 * (eps * np.abs(o) + (e32 + (eps if typ != torch.float32 else 0)) * pv) + 2.0 ** -126 * (sv + 1)
+            assert (np.abs(h["att"][row, head] - o) <= tol).all()
+        w = olm.verify_drafts(h["logits"], host(draft), host(tokens), host(parents), host(offsets), before["lens"], host(accept),
+                              host(sample), 0.8, 1.0, False, R * n)
+        assert w[3] > 2.0 ** -16 and w[4] > 2.0 ** -45
+        for g, x in zip(got, w):
+            np.testing.assert_array_equal(g, x)
+        tab, fr, off, _, st = olm.block_tables(before["lens"], w[0], before["table"], before["free"], B, R * n)
+        assert st[0] == 0 and (host(table) == tab).all() and (host(free) == fr).all() and (host(first) == off).all()
+        c = olm.cache8_append(h["k"], h["v"], before["kc"], before["vc"], before["ks"], before["vs"], tab, before["lens"], off,
+                              w[1][:off[-1]], "f32" if typ == torch.float32 else "bf16")
+        for t, x in zip((kc, vc, ks, vs), c):
+            np.testing.assert_array_equal(host(t), x)
+        total += int((w[0] - before["lens"] > 1).sum())
+        lens.copy_(kept["got"].new_len)
+        last = got[2]
+    assert total > 5

@@ -531,6 +531,51 @@ struct Share {
   }
 };
 
+// Where the workgroup's share begins: its units and the place of its first part;
+// s_begin has the request and the units before that.  False if there are none.
+template <int TP, int NW>
+__device__ __forceinline__ bool share_begin(const AttnDev& p, int (&s_wave)[NW], int (&s_begin)[2], int* unit, int* end, int* part) {
+  constexpr int THREADS = 64 * NW;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, n_req = p.a.n_req;
+  // each thread's requests, then the sums of those before them
+  const int some = (n_req + THREADS - 1) / THREADS;
+  int mine = 0;
+  for (int x = tid * some; x < (tid + 1) * some && x < n_req; ++x) mine += Share::units(p, x, TP);
+  int run = mine;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int up = __shfl_up(run, d, 64);
+    if (lane >= d) run += up;
+  }
+  if (lane == 63) s_wave[wave] = run;
+  __syncthreads();
+  int all = 0, pre = run - mine;
+#pragma unroll
+  for (int x = 0; x < NW; ++x) {
+    if (x < wave) pre += s_wave[x];
+    all += s_wave[x];
+  }
+  // workgroups on one XCD (every eighth) take neighbouring units
+  const int g = (int)(blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8), per = Share::per(p, all);
+  const int u0 = g * per, u1 = min(all, u0 + per);
+  for (int x = tid * some; x < (tid + 1) * some && x < n_req; ++x) {
+    const int u = Share::units(p, x, TP);
+    if (blockIdx.x == 0) p.first_unit[x] = pre;
+    if (u0 >= pre && u0 < pre + u) {
+      s_begin[0] = x;
+      s_begin[1] = pre;
+    }
+    pre += u;
+  }
+  if (blockIdx.x == 0 && tid == 0) p.first_unit[n_req] = all;
+  if (u0 >= u1) return false;
+  *unit = u0;
+  *end = u1;
+  *part = 2 * g;
+  __syncthreads();
+  return true;
+}
+
 }  // namespace
 
 // Few rows: a workgroup takes 16 rows of one request and key head against one
@@ -544,211 +589,254 @@ struct Share {
 // requests of 1000 to 2000, one row a head, 4 key heads of 128, bf16: 0.6 GB in
 // 131 us).  Small calls are bound by the chain of table entry, K, scores, V (64 drafts
 // of up to 8 nodes over at most 120 tokens, 4 heads of 32, fp32: 8.5 us).
-constexpr int resident8(int type, int dp) {
+
+// Waves of a SIMD that its registers are for, of 8-bit caches; of shared work few enough
+// that nothing of the loop around the items goes to scratch memory.
+constexpr int resident8(int type, int dp, bool share) {
+  if (share) return dp <= 64 ? (type == MCA_TYPE_F32 ? 2 : 3) : (dp <= 128 ? 2 : 1);
   return dp <= 64 ? (type == MCA_TYPE_F32 ? 3 : 4) : (dp <= 128 ? (type == MCA_TYPE_F32 ? 2 : 3) : 1);
 }
-template <int TYPE, int DP, bool PAD, bool C8>
-__global__ __launch_bounds__(kAttnThreads, C8 ? resident8(TYPE, DP) : 1) void k_lm_attn(AttnDev p) {
+template <int TYPE, int DP, bool PAD, bool C8, bool SHARE = false>
+__global__ __launch_bounds__(kAttnThreads, C8 ? resident8(TYPE, DP, SHARE) : 1) void k_lm_attn(AttnDev args) {
   constexpr int LB = DP / 4 < 16 ? DP / 4 : 16;  // bytes of a load of 8-bit keys
   typedef Rows<TYPE, DP, 1, 1, PAD, C8 ? LB : 0> R;
   constexpr int EL = R::EL, KL = R::KL, VD = R::VD, CD = R::CD, NC = R::NC, OT = R::OT;
-  const mca_tree_attention_args& a = p.a;
   __shared__ int s_par[2][MCA_MAX_NODES];
   __shared__ uint32_t s_mask[2][MCA_MAX_NODES][kMaskWords];
   __shared__ float s_o[2][OT * 4][64];
   __shared__ float s_ml[2][2][64];
+  __shared__ int s_wave[kAttnWaves], s_begin[2];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  int rt, h, r, split, first, n;
-  if (!place(p, &rt, &h, &r, &split) || !rows_of(a, r, &first, &n)) return;
-  const int row0 = rt * 16;
-  if (row0 >= n * p.group) return;
-  const int len = cached_of(a, r), nchunk = chunks_of(len, p.chunk);
-  if (split >= nchunk) return;
-  R w;
-  w.begin(a, h, p.group, row0, n * p.group, first, n);
-  const int q = w.q, li = w.li;
-  u32x4 kf[2][KL];
-  uint32_t vf[8][VD];
-  // the tile's tokens: token (lane & 31) is row `row` of kb and vb
-  auto load_tile = [&](int row, const char* kb, uint32_t ks, const char* vb, uint32_t vs) {
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const char* kp = kb + (uint64_t)(uint32_t)__shfl(row, 16 * x + li, 64) * ks;
-#pragma unroll
-      for (int i = 0; i < KL; ++i)
-        kf[x][i] = (!PAD || w.part_at(i, q) < w.dbytes) ? gload((const u32x4*)(kp + w.part_at(i, q))) : u32x4{0, 0, 0, 0};
+  constexpr int TP = kAttnWaves * kTilePos;  // tokens of a unit of shared work
+  constexpr bool shared = SHARE;
+  int rt = 0, h = 0, r = 0, split = 0, first, n;
+  int unit = 0, unit_end = 0, before = 0, part = 0;
+  if (shared) {
+    if (!share_begin<TP, kAttnWaves>(again(), s_wave, s_begin, &unit, &unit_end, &part)) return;
+    r = __builtin_amdgcn_readfirstlane(s_begin[0]);
+    before = __builtin_amdgcn_readfirstlane(s_begin[1]);
+  } else if (!place(args, &rt, &h, &r, &split)) {
+    return;
+  }
+  // one item, or those of the workgroup's share
+  while (true) {
+    const AttnDev& p = SHARE ? again() : args;
+    const mca_tree_attention_args& a = p.a;
+    int from_token, end, parts;  // the cached tokens, and in how many parts the rows are worked on
+    bool drafted;
+    if (shared) {
+      if (unit >= unit_end) return;
+      for (int units = Share::units(p, r, TP); unit >= before + units; units = Share::units(p, r, TP)) {
+        before += units;
+        ++r;
+      }
+      rows_of(a, r, &first, &n);
+      const int len = cached_of(a, r);
+      const Share sh(p, len, n, TP);
+      h = (unit - before) / sh.tiles;
+      const int tile0 = unit - before - h * sh.tiles, tile1 = min(sh.tiles, tile0 + (unit_end - unit));
+      unit += tile1 - tile0;
+      from_token = tile0 * TP;
+      end = min(len, tile1 * TP);
+      drafted = tile1 * TP > len && tile1 == sh.tiles;
+      parts = tile0 == 0 && tile1 == sh.tiles ? 1 : 2;
+    } else {
+      if (!rows_of(a, r, &first, &n) || rt * 16 >= n * p.group) return;
+      const int len = cached_of(a, r);
+      parts = chunks_of(len, p.chunk);
+      if (split >= parts) return;
+      from_token = split * p.chunk;
+      end = min(len, (split + 1) * p.chunk);
+      drafted = split == parts - 1;
     }
+    const int row0 = rt * 16;
+    R w;
+    w.begin(a, h, p.group, row0, n * p.group, first, n);
+    const int q = w.q, li = w.li;
+    u32x4 kf[2][KL];
+    uint32_t vf[8][VD];
+    // the tile's tokens: token (lane & 31) is row `row` of kb and vb
+    auto load_tile = [&](int row, const char* kb, uint32_t ks, const char* vb, uint32_t vs) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const char* vp = vb + (uint64_t)(uint32_t)__shfl(row, 4 * q + (j & 3) + 16 * (j >> 2), 64) * vs + li * CD * 4;
+      for (int x = 0; x < 2; ++x) {
+        const char* kp = kb + (uint64_t)(uint32_t)__shfl(row, 16 * x + li, 64) * ks;
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if (!PAD || (c * 16 + li) * CD * 4 < w.dbytes) {
-          load_words<CD>(vp + c * 64 * CD, &vf[j][c * CD]);
-        } else {
+        for (int i = 0; i < KL; ++i)
+          kf[x][i] = (!PAD || w.part_at(i, q) < w.dbytes) ? gload((const u32x4*)(kp + w.part_at(i, q))) : u32x4{0, 0, 0, 0};
+      }
 #pragma unroll
-          for (int d = 0; d < CD; ++d) vf[j][c * CD + d] = 0;
+      for (int j = 0; j < 8; ++j) {
+        const char* vp = vb + (uint64_t)(uint32_t)__shfl(row, 4 * q + (j & 3) + 16 * (j >> 2), 64) * vs + li * CD * 4;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          if (!PAD || (c * 16 + li) * CD * 4 < w.dbytes) {
+            load_words<CD>(vp + c * 64 * CD, &vf[j][c * CD]);
+          } else {
+#pragma unroll
+            for (int d = 0; d < CD; ++d) vf[j][c * CD + d] = 0;
+          }
         }
       }
-    }
-  };
-  auto scores = [&]() {
+    };
+    auto scores = [&]() {
 #pragma unroll
-    for (int x = 0; x < 2; ++x) w.score(x, [&](int i) { return kf[x][i]; });
-  };
-  uint32_t see[1][1];
-  {
-    const int32_t* tab = a.table + (int64_t)r * a.table_stride;
-    const int end = min(len, (split + 1) * p.chunk);
-    int p0 = split * p.chunk + wave * kTilePos;
-    int blk = p0 < end ? cache_block(a, tab, p0 + (lane & 31), end) : 0;
-    if constexpr (C8) {
-      // A tile's codes are requested while the one before is worked on (a value takes
-      // half the registers that it would in 16 bits), and widened, times its block's
-      // scale, where its product takes it.
-      constexpr int NK = DP / 4 / LB, VB = CD * 4 / EL, VW = VB < 4 ? 1 : VB / 4;  // loads of a K row, bytes and words of one of V
-      uint32_t kc[2][NK][LB / 4], vc[8][NC][VW], nk[2][NK][LB / 4], nv[8][NC][VW];
-      int row = -1, ks = 0, vs = 0;
-      auto request = [&](int at) {
-        row = cache_row(a, blk, h, at + (lane & 31), end);
-        const int of = row >= 0 ? blk * a.n_kv_head + h : 0, from = max(row, 0);
-        ks = gload(p.k_scale + of);
-        vs = gload(p.v_scale + of);
+      for (int x = 0; x < 2; ++x) w.score(x, [&](int i) { return kf[x][i]; });
+    };
+    uint32_t see[1][1];
+    {
+      const int32_t* tab = a.table + (int64_t)r * a.table_stride;
+      int p0 = from_token + wave * kTilePos;
+      int blk = p0 < end ? cache_block(a, tab, p0 + (lane & 31), end) : 0;
+      if constexpr (C8) {
+        // A tile's codes are requested while the one before is worked on (a value takes
+        // half the registers that it would in 16 bits), and widened, times its block's
+        // scale, where its product takes it.
+        constexpr int NK = DP / 4 / LB, VB = CD * 4 / EL, VW = VB < 4 ? 1 : VB / 4;  // loads of a K row, bytes and words of one of V
+        uint32_t kc[2][NK][LB / 4], vc[8][NC][VW], nk[2][NK][LB / 4], nv[8][NC][VW];
+        int row = -1, ks = 0, vs = 0;
+        auto request = [&](int at) {
+          row = cache_row(a, blk, h, at + (lane & 31), end);
+          const int of = row >= 0 ? blk * a.n_kv_head + h : 0, from = max(row, 0);
+          ks = gload(p.k_scale + of);
+          vs = gload(p.v_scale + of);
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const char* kp = (const char*)a.k_cache + (uint64_t)(uint32_t)__shfl(from, 16 * x + li, 64) * a.head_dim + LB * q;
+          for (int x = 0; x < 2; ++x) {
+            const char* kp = (const char*)a.k_cache + (uint64_t)(uint32_t)__shfl(from, 16 * x + li, 64) * a.head_dim + LB * q;
 #pragma unroll
-          for (int i = 0; i < NK; ++i) {
-            if (!PAD || 4 * LB * i + LB * q < a.head_dim) {
-              load_codes<LB>(kp + 4 * LB * i, nk[x][i]);
-            } else {
+            for (int i = 0; i < NK; ++i) {
+              if (!PAD || 4 * LB * i + LB * q < a.head_dim) {
+                load_codes<LB>(kp + 4 * LB * i, nk[x][i]);
+              } else {
 #pragma unroll
-              for (int d = 0; d < LB / 4; ++d) nk[x][i][d] = 0;
+                for (int d = 0; d < LB / 4; ++d) nk[x][i][d] = 0;
+              }
             }
           }
-        }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const char* vp = (const char*)a.v_cache + (uint64_t)(uint32_t)__shfl(from, 4 * q + (j & 3) + 16 * (j >> 2), 64) * a.head_dim + VB * li;
+          for (int j = 0; j < 8; ++j) {
+            const char* vp = (const char*)a.v_cache + (uint64_t)(uint32_t)__shfl(from, 4 * q + (j & 3) + 16 * (j >> 2), 64) * a.head_dim + VB * li;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) {
-            if (!PAD || (c * 16 + li) * VB < a.head_dim) {
-              load_codes<VB>(vp + c * 16 * VB, nv[j][c]);
-            } else {
+            for (int c = 0; c < NC; ++c) {
+              if (!PAD || (c * 16 + li) * VB < a.head_dim) {
+                load_codes<VB>(vp + c * 16 * VB, nv[j][c]);
+              } else {
 #pragma unroll
-              for (int d = 0; d < VW; ++d) nv[j][c][d] = 0;
+                for (int d = 0; d < VW; ++d) nv[j][c][d] = 0;
+              }
             }
           }
-        }
-        blk = cache_block(a, tab, at + kAttnWaves * kTilePos + (lane & 31), end);
-      };
-      if (p0 < end) request(p0);
-      for (; p0 < end; p0 += kAttnWaves * kTilePos) {
-        const uint32_t valid = (uint32_t)__ballot(row >= 0);
-        const int ksc = ks, vsc = vs;
+          blk = cache_block(a, tab, at + kAttnWaves * kTilePos + (lane & 31), end);
+        };
+        if (p0 < end) request(p0);
+        for (; p0 < end; p0 += kAttnWaves * kTilePos) {
+          const uint32_t valid = (uint32_t)__ballot(row >= 0);
+          const int ksc = ks, vsc = vs;
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+          for (int x = 0; x < 2; ++x)
 #pragma unroll
-          for (int i = 0; i < NK; ++i)
+            for (int i = 0; i < NK; ++i)
 #pragma unroll
-            for (int d = 0; d < LB / 4; ++d) kc[x][i][d] = nk[x][i][d];
+              for (int d = 0; d < LB / 4; ++d) kc[x][i][d] = nk[x][i][d];
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int c = 0; c < NC; ++c)
-#pragma unroll
-            for (int d = 0; d < VW; ++d) vc[j][c][d] = nv[j][c][d];
-        if (p0 + kAttnWaves * kTilePos < end) request(p0 + kAttnWaves * kTilePos);
-        see[0][0] = valid;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const float f = scale_of((uint32_t)__shfl(ksc, 16 * x + li, 64));
-          constexpr int PP = LB * EL / 16, PC = 16 / EL / 4;  // parts of a load, words of codes of a part
-          w.score(x, [&](int i) { return wide_part<TYPE>(&kc[x][i / PP][i % PP * PC], f); });
-        }
-        w.weigh(valid == 0xffffffffu, see);
-        float f[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          f[j] = scale_of((uint32_t)__shfl(vsc, 4 * q + (j & 3) + 16 * (j >> 2), 64));
-          if (valid != 0xffffffffu) {
-            const bool ok = (valid >> (4 * q + (j & 3) + 16 * (j >> 2))) & 1;
+          for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
 #pragma unroll
-              for (int d = 0; d < VW; ++d) vc[j][c][d] = ok ? vc[j][c][d] : 0u;
+              for (int d = 0; d < VW; ++d) vc[j][c][d] = nv[j][c][d];
+          if (p0 + kAttnWaves * kTilePos < end) request(p0 + kAttnWaves * kTilePos);
+          see[0][0] = valid;
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float f = scale_of((uint32_t)__shfl(ksc, 16 * x + li, 64));
+            constexpr int PP = LB * EL / 16, PC = 16 / EL / 4;  // parts of a load, words of codes of a part
+            w.score(x, [&](int i) { return wide_part<TYPE>(&kc[x][i / PP][i % PP * PC], f); });
           }
+          w.weigh(valid == 0xffffffffu, see);
+          float f[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            f[j] = scale_of((uint32_t)__shfl(vsc, 4 * q + (j & 3) + 16 * (j >> 2), 64));
+            if (valid != 0xffffffffu) {
+              const bool ok = (valid >> (4 * q + (j & 3) + 16 * (j >> 2))) & 1;
+#pragma unroll
+              for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int d = 0; d < VW; ++d) vc[j][c][d] = ok ? vc[j][c][d] : 0u;
+            }
+          }
+          w.add_words(0, [&](int j, int d) {
+            const int c = d / CD, x = d % CD;
+            if constexpr (TYPE == MCA_TYPE_F32)
+              return x & 2 ? wide2_f32<true>(vc[j][c][0], f[j])[x & 1] : wide2_f32<false>(vc[j][c][0], f[j])[x & 1];
+            else
+              return x & 1 ? wide2<TYPE, true>(vc[j][c][x / 2], f[j]) : wide2<TYPE, false>(vc[j][c][x / 2], f[j]);
+          });
         }
-        w.add_words(0, [&](int j, int d) {
-          const int c = d / CD, x = d % CD;
-          if constexpr (TYPE == MCA_TYPE_F32)
-            return x & 2 ? wide2_f32<true>(vc[j][c][0], f[j])[x & 1] : wide2_f32<false>(vc[j][c][0], f[j])[x & 1];
-          else
-            return x & 1 ? wide2<TYPE, true>(vc[j][c][x / 2], f[j]) : wide2<TYPE, false>(vc[j][c][x / 2], f[j]);
-        });
+      } else {
+        for (; p0 < end; p0 += kAttnWaves * kTilePos) {
+          const int row = cache_row(a, blk, h, p0 + (lane & 31), end);
+          blk = cache_block(a, tab, p0 + kAttnWaves * kTilePos + (lane & 31), end);
+          const uint32_t valid = (uint32_t)__ballot(row >= 0);
+          load_tile(max(row, 0), (const char*)a.k_cache, w.dbytes, (const char*)a.v_cache, w.dbytes);
+          see[0][0] = valid;
+          if (valid != 0xffffffffu) w.clear(vf, valid);
+          scores();
+          w.weigh(valid == 0xffffffffu, see);
+          w.add(0, vf);
+        }
       }
-    } else {
-      for (; p0 < end; p0 += kAttnWaves * kTilePos) {
-        const int row = cache_row(a, blk, h, p0 + (lane & 31), end);
-        blk = cache_block(a, tab, p0 + kAttnWaves * kTilePos + (lane & 31), end);
-        const uint32_t valid = (uint32_t)__ballot(row >= 0);
-        load_tile(max(row, 0), (const char*)a.k_cache, w.dbytes, (const char*)a.v_cache, w.dbytes);
-        see[0][0] = valid;
-        if (valid != 0xffffffffu) w.clear(vf, valid);
+    }
+    if (drafted) {
+      const int from = ancestors(a.parents + first, n, s_par, s_mask);
+      const int n0 = kTilePos * wave;
+      if (n0 < n) {
+        const int nd = n0 + (lane & 31);
+        const uint32_t valid = (uint32_t)__ballot(nd < n);
+        const char* kb = (const char*)a.k + ((int64_t)first * a.k_row + (int64_t)h * a.k_head) * EL;
+        const char* vb = (const char*)a.v + ((int64_t)first * a.v_row + (int64_t)h * a.v_head) * EL;
+        load_tile(nd < n ? nd : 0, kb, (uint32_t)(a.k_row * EL), vb, (uint32_t)(a.v_row * EL));
+        see[0][0] = s_mask[from][min(w.node[0], n - 1)][wave];
+        const uint32_t odd = w.odd_of(vf) & valid;
+        w.clear(vf, valid & ~odd);
         scores();
-        w.weigh(valid == 0xffffffffu, see);
+        w.weigh(false, see);
         w.add(0, vf);
+        w.add_odd(0, odd, see, [&](int at) { return vb + (int64_t)(n0 + at) * a.v_row * EL; });
       }
     }
-  }
-  if (split == nchunk - 1) {
-    const int from = ancestors(a.parents + first, n, s_par, s_mask);
-    const int n0 = kTilePos * wave;
-    if (n0 < n) {
-      const int nd = n0 + (lane & 31);
-      const uint32_t valid = (uint32_t)__ballot(nd < n);
-      const char* kb = (const char*)a.k + ((int64_t)first * a.k_row + (int64_t)h * a.k_head) * EL;
-      const char* vb = (const char*)a.v + ((int64_t)first * a.v_row + (int64_t)h * a.v_head) * EL;
-      load_tile(nd < n ? nd : 0, kb, (uint32_t)(a.k_row * EL), vb, (uint32_t)(a.v_row * EL));
-      see[0][0] = s_mask[from][min(w.node[0], n - 1)][wave];
-      const uint32_t odd = w.odd_of(vf) & valid;
-      w.clear(vf, valid & ~odd);
-      scores();
-      w.weigh(false, see);
-      w.add(0, vf);
-      w.add_odd(0, odd, see, [&](int at) { return vb + (int64_t)(n0 + at) * a.v_row * EL; });
+    // join the waves: 2, 3 into 0, 1, then 1 into 0
+    w.sum_lanes();
+#pragma unroll
+    for (int half = kAttnWaves / 2; half > 0; half >>= 1) {
+      __syncthreads();
+      if (wave >= half && wave < 2 * half) {
+        s_ml[wave - half][0][lane] = w.m[0];
+        s_ml[wave - half][1][lane] = w.l[0];
+#pragma unroll
+        for (int e = 0; e < OT; ++e)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) s_o[wave - half][e * 4 + v][lane] = w.o[0][e][v];
+      }
+      __syncthreads();
+      if (wave < half) {
+        const float m2 = s_ml[wave][0][lane], l2 = s_ml[wave][1][lane];
+        const float mn = fmaxf(w.m[0], m2);
+        const float f1 = __builtin_amdgcn_exp2f(w.m[0] - mn), f2 = __builtin_amdgcn_exp2f(m2 - mn);
+        w.m[0] = mn;
+        w.l[0] = w.l[0] * f1 + l2 * f2;
+#pragma unroll
+        for (int e = 0; e < OT; ++e)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) w.o[0][e][v] = w.o[0][e][v] * f1 + s_o[wave][e * 4 + v][lane] * f2;
+      }
     }
+    if (wave == 0)
+      w.write(p, parts == 1, [&](int t) {
+        return shared ? (int64_t)part * p.rows + li : ((int64_t)(first + w.node[t]) * a.n_head + w.head[t]) * p.splits + split;
+      });
+    if (!shared) return;
+    part |= 1;  // a workgroup's later items are its last, if they are cut
   }
-  // join the waves: 2, 3 into 0, 1, then 1 into 0
-  w.sum_lanes();
-#pragma unroll
-  for (int half = kAttnWaves / 2; half > 0; half >>= 1) {
-    __syncthreads();
-    if (wave >= half && wave < 2 * half) {
-      s_ml[wave - half][0][lane] = w.m[0];
-      s_ml[wave - half][1][lane] = w.l[0];
-#pragma unroll
-      for (int e = 0; e < OT; ++e)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) s_o[wave - half][e * 4 + v][lane] = w.o[0][e][v];
-    }
-    __syncthreads();
-    if (wave < half) {
-      const float m2 = s_ml[wave][0][lane], l2 = s_ml[wave][1][lane];
-      const float mn = fmaxf(w.m[0], m2);
-      const float f1 = __builtin_amdgcn_exp2f(w.m[0] - mn), f2 = __builtin_amdgcn_exp2f(m2 - mn);
-      w.m[0] = mn;
-      w.l[0] = w.l[0] * f1 + l2 * f2;
-#pragma unroll
-      for (int e = 0; e < OT; ++e)
-#pragma unroll
-        for (int v = 0; v < 4; ++v) w.o[0][e][v] = w.o[0][e][v] * f1 + s_o[wave][e * 4 + v][lane] * f2;
-    }
-  }
-  if (wave == 0)
-    w.write(p, nchunk == 1, [&](int t) {
-      return ((int64_t)(first + w.node[t]) * a.n_head + w.head[t]) * p.splits + split;
-    });
 }
 
 // Many rows: each of the NW waves takes 16 QT rows of its own, and all read the
@@ -1157,11 +1245,11 @@ __global__ __launch_bounds__(256) void k_lm_attn_join(AttnDev p) {
 // rows, which are cut in the same places, 4 at a time: their weights are made in
 // LDS, then its NW waves take parts in turn and are added there.  head_dim is at
 // most 64 NI.
-constexpr int kMaxSharers = 512;
-template <int TYPE, int NI, int NW>
+constexpr int kMaxSharers = 512, kMaxSharers8 = 1024;  // workgroups, and those of the narrow kernel
+template <int TYPE, int NI, int NW, int SHARERS>
 __global__ __launch_bounds__(64 * NW) void k_lm_attn_join_shared(AttnDev p, int TP, int fours) {
   const mca_tree_attention_args& a = p.a;
-  __shared__ float s_w[4][kMaxSharers];
+  __shared__ float s_w[4][SHARERS];
   __shared__ float s_acc[NW][4 * 64 * NI];
   const int groups = p.rows / (4 * fours), tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int tile = blockIdx.x / groups, rt = tile % p.row_tiles, rh = tile / p.row_tiles;
@@ -1314,6 +1402,11 @@ void launch_pad(const AttnDev& p, dim3 grid, hipStream_t s) {
   constexpr bool kBig = DP > (TYPE == MCA_TYPE_F32 ? 64 : 128);             // big_rows()
   constexpr bool kEight = TYPE == MCA_TYPE_F32 ? DP == 128 : DP >= 128;     // wide_waves() may be 8
   if (!is_wide<C8>(p.a)) {
+    if constexpr (C8)
+      if (p.sharers > 0) {
+        hipLaunchKernelGGL((k_lm_attn<TYPE, DP, PAD, C8, true>), grid, dim3(kAttnThreads), 0, s, p);
+        return;
+      }
     hipLaunchKernelGGL((k_lm_attn<TYPE, DP, PAD, C8>), grid, dim3(kAttnThreads), 0, s, p);
     return;
   }
@@ -1342,10 +1435,12 @@ void launch_dim(const AttnDev& p, dim3 grid, hipStream_t s) {
 // 8192, 128 rows, head_dim 128, 512 workgroups, 58 and 54).
 template <int TYPE, int NI, bool C8>
 void launch_join(const AttnDev& p, dim3 groups, int fours, hipStream_t s) {
+  constexpr int SHARERS = C8 ? kMaxSharers8 : kMaxSharers;
+  const int tokens = is_wide<C8>(p.a) ? tile_tokens(p.a) : kAttnWaves * kTilePos;
   if (groups.x <= kCUs)
-    hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 16>), groups, dim3(1024), 0, s, p, tile_tokens(p.a), fours);
+    hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 16, SHARERS>), groups, dim3(1024), 0, s, p, tokens, fours);
   else
-    hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 4>), groups, dim3(256), 0, s, p, tile_tokens(p.a), fours);
+    hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 4, SHARERS>), groups, dim3(256), 0, s, p, tokens, fours);
 }
 template <int TYPE, bool C8>
 void launch_type(const AttnDev& p, dim3 grid, hipStream_t s) {
@@ -1401,6 +1496,24 @@ AttnPlan attention_plan(const mca_tree_attention_args& a) {
       p.bytes = ((size_t)a.n_req + 1 + 63) / 64 * 256 + (size_t)2 * p.sharers * tile_rows<C8>(a) * (a.head_dim + 1) * sizeof(float);
     }
     return p;
+  }
+  if (C8 && row_tiles<C8>(a) == 1 && a.head_dim > 64) {
+    // Shared, over long contexts: the chunks of ragged ones leave the chip idle behind the
+    // last (chunks and shares, us, one row or four a head, 8 key heads of 128, bf16: 32 of
+    // 8192 to 32768 271 and 259, 8 of 100000 218 and 190, one 64 and 53; but 256 of 2000 154
+    // and 169, 8 of 8000 32 and 39, and head_dim 64, 32 of 32768 142 and 146).  Wider fp32
+    // rows, whose chunks' kernel works in scratch memory, always: 32 of 8192 531 and 364, of
+    // 1000 131 and 108.
+    const bool big = a.dtype == MCA_TYPE_F32 && a.head_dim > 128;
+    const int64_t units = wgs * ((a.max_len + kAttnWaves * kTilePos - 1) / (kAttnWaves * kTilePos) + 1);
+    const int resident = kCUs * resident8(a.dtype, a.head_dim, true);
+    if ((big || a.max_len >= 1 << 14) && units >= 8 * resident && units < (1 << 30)) {
+      p.chunk = a.max_len;
+      p.splits = 1;
+      p.sharers = resident;
+      p.bytes = ((size_t)a.n_req + 1 + 63) / 64 * 256 + (size_t)2 * p.sharers * 16 * (a.head_dim + 1) * sizeof(float);
+      return p;
+    }
   }
   // Chunks of at least two tiles a wave while there are fewer than two workgroups a
   // CU; behind that of 1536 tokens, up to 16 workgroups a CU, which evens out requests

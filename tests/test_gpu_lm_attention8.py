@@ -104,6 +104,23 @@ def test_many_rows(lm, typ, dim, rows):
     check(s, lm.mca_tree_attention8(**s, max_len=LONG))
 
 
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("dim,nodes,group", [(80, 1, 1), (128, 1, 8), (128, 4, 4), (128, 16, 1), (256, 3, 2), (240, 1, 1)])
+def test_shares_of_few_rows(lm, typ, dim, nodes, group):
+    """At most 16 rows a key head whose max_len lets the work be dealt out: requests that one workgroup has whole, cut at
+    its ends, over several of them, without cached tokens, without nodes."""
+    lens = [900, 0, 77, 2600, 5, 1300, 128, 3, 3, 3, 500, 1024]
+    s = make(dim + nodes, typ, lens, [nodes, nodes, 1, nodes, 0] + [nodes] * 7, 2 * group, 2, dim, 50, spread=3)
+    keep = torch.full_like(s["q"], 5.0), torch.full(s["q"].shape[:2], 6.0, device="cuda")
+    got = lm.mca_tree_attention8(**s, max_len=LONG, out=keep[0], lse=keep[1])
+    used = check(s, got)
+    assert (host(got[0])[~used] == 5).all()
+    table = host(s["table"])
+    table[3, 7], table[0, 3:5] = -1, 10 ** 6  # blocks that are not there
+    s["table"] = put(table)
+    check(s, lm.mca_tree_attention8(**s, max_len=LONG))
+
+
 @pytest.mark.parametrize("typ", ["bf16", "f32"])
 def test_split_over_one_request(lm, typ):
     """Few rows over a long context, in chunks that are joined."""

@@ -161,7 +161,7 @@ int mca_tree_attention(const mca_tree_attention_args* args, void* hip_stream);
  * outside [0, n_src) counts as zeros.  Blocks outside [0, n_blocks), positions
  * behind max_blocks, and requests of negative lengths or of offsets out of range are
  * left as they were, and places behind a request's last token are.  Requests share no
- * blocks.  The call with the same arguments again gives the same results once more. */
+ * blocks, and offsets do not fall.  The call with the same arguments again gives the same results once more. */
 typedef struct mca_cache8_append_args {
   int32_t dtype, n_req, n_kv_head, head_dim, block_size, n_blocks, max_blocks, reserved;
   int64_t n, n_src, table_stride;
@@ -236,11 +236,11 @@ int mca_tree_attention8(const mca_tree_attention8_args* args, void* hip_stream);
  * (mca_block_tables' new_len, mca_cache_append's and mca_cache8_append's rows); token
  * [n_req] the tokens that follow.  A child whose token is outside [0, n_vocab) is
  * not accepted and changes nothing.  At a node whose target row (or draft row, if it
- * has children) has no softmax (NaN, +inf, nothing but -inf, also after the scale),
+ * has children) has no softmax (NaN, +inf, nothing but -inf),
  * the path ends and token is -1; so it is for requests without nodes, of more than
  * max_nodes or of offsets out of range, whose new_len is lengths[r].
- * Sums and borders are computed in 64 bits from exponentials of 32 where a child is
- * tried and of 64 where a token is drawn. */
+ * Sums are held in 64 bits, of exponentials of 32 where a child is tried and of 64 where
+ * a token is drawn (there c is a sum of such ones, too). */
 typedef struct mca_verify_drafts_args {
   int32_t dtype, n_req, max_nodes, greedy;
   int64_t n_rows, n_vocab, target_row, draft_row;

@@ -106,19 +106,22 @@ __device__ __forceinline__ void unpack(u32x4 x, float (&f)[Elem<TYPE>::kPer]) {
 // Exponentials and logarithms of 64 bits (the library's are made for all numbers).
 // exp(x) of N numbers of at most 700, to 2^-47: 2^n times the series of exp in the rest,
 // which is at most ln 2 / 2, to its 11th power.  Results below 2^-1021 are 0, NaN stays.
-// The steps of several go side by side: one by one, each would wait for the one before.
+// n comes from the last bits of x / ln 2 + 1.5 2^52 and goes into the exponent as bits:
+// conversions, roundings and ldexp of 64 bits take four times as long as a sum.  The steps
+// of several go side by side: one by one, each would wait for the one before.
 template <int N>
 __device__ __forceinline__ void exps_of(double (&x)[N]) {
   constexpr double kInvLn2 = 1.4426950408889634074, kLn2 = 0.69314718055994530942, kLn2Rest = 2.3190468138462996e-17;
+  constexpr double kBits = 0x1.8p52;
   constexpr double kOver[12] = {1.0,          1.0,           1.0 / 2,        1.0 / 6,         1.0 / 24,         1.0 / 120,
                                 1.0 / 720,    1.0 / 5040,    1.0 / 40320,    1.0 / 362880,    1.0 / 3628800,    1.0 / 39916800};  // 1 / k!
-  double n[N], r[N], y[N];
+  double t[N], r[N], y[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) n[i] = __builtin_rint(x[i] * kInvLn2);
+  for (int i = 0; i < N; ++i) t[i] = fma(x[i], kInvLn2, kBits);
 #pragma unroll
-  for (int i = 0; i < N; ++i) r[i] = fma(n[i], -kLn2, x[i]);
+  for (int i = 0; i < N; ++i) r[i] = fma(t[i] - kBits, -kLn2, x[i]);
 #pragma unroll
-  for (int i = 0; i < N; ++i) r[i] = fma(n[i], -kLn2Rest, r[i]);
+  for (int i = 0; i < N; ++i) r[i] = fma(t[i] - kBits, -kLn2Rest, r[i]);
 #pragma unroll
   for (int i = 0; i < N; ++i) y[i] = kOver[11];
 #pragma unroll
@@ -128,7 +131,11 @@ __device__ __forceinline__ void exps_of(double (&x)[N]) {
     if constexpr (N > 1) __builtin_amdgcn_sched_barrier(0);
   }
 #pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = x[i] < -708.0 ? 0.0 : __builtin_ldexp(y[i], (int)n[i]);
+  for (int i = 0; i < N; ++i) {
+    const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, t[i]);
+    const uint64_t bits = __builtin_bit_cast(uint64_t, y[i]) + ((uint64_t)(n << 20) << 32);
+    x[i] = x[i] < -707.0 ? 0.0 : __builtin_bit_cast(double, bits);
+  }
 }
 __device__ __forceinline__ double exp_of(double x) {
   double y[1] = {x};

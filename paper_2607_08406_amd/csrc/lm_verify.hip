@@ -10,7 +10,14 @@
 // ends at the sums again in 64 bits and the draw.  The draw compares a random number
 // with sums over the vocabulary, whose borders lie close: exponentials of 32 bits move
 // them by 1e-8, which at 128000 symbols would give another token once in a thousand draws,
-// those of 64 by 1e-16.
+// those of 64 by 1e-14.  So where children were rejected at that node, c is made again from
+// sums of 64 bits, one step of all of the chip for each of the first rejections.
+//
+// What bounds it: only the first step moves many bytes.  The others are chains of short
+// kernels, whose time is their launch, the spread of their workgroups and 64-bit
+// arithmetic (about 25 operations a symbol).  bf16, 32 requests of up to 9 nodes, 128000
+// symbols: rows 21 us (82 MB, 3.9 TB/s), walk 25, sums 11, draw 24, its further steps 16, 4
+// and 3: 100 us in a graph.
 #include <algorithm>
 
 #include "device_common.hpp"
@@ -27,8 +34,9 @@ constexpr int kWalkThreads = 1024;  // of the walk over large vocabularies, whos
 constexpr int kVUnroll = 4;
 constexpr int kVMaxSplits = 64;   // parts of a row
 constexpr int64_t kVPart = 8192;  // symbols of a part at least
+constexpr int kVSteps = 3;        // further steps of the draw
 constexpr int kVSide = 8;         // symbols side by side in a thread of the draw
-constexpr int kVCut = 4096;       // symbols of a cut of the draw, but for very large vocabularies
+constexpr int kVCut = 2048;       // symbols of a cut of the draw at least
 constexpr int kVSegment = 256;    // symbols that a wave weighs at a time in the kernel of whole requests
 constexpr int kVWhole = 32 * kVSegment;  // its largest vocabulary (64 segments at most)
 constexpr float kLowest = -3.402823466e38f;
@@ -43,9 +51,10 @@ struct RowPart {
 // Where a request's path ends: what its token is drawn from.
 struct End {
   int64_t row;  // of the logits; -1: no token
-  double c;     // 0: p alone
+  double c;     // 0: p alone; 1 behind the first rejection
   float mp, mq;  // largest logits
-  int32_t first, node, gone, reserved;  // given drafts: this many of the node's children were rejected
+  int32_t first, node, gone;  // given drafts: the children before this one were rejected
+  int32_t more;               // drawn ones: rejections whose S is still to be added to c
 };
 
 struct VerifyDev {
@@ -56,6 +65,7 @@ struct VerifyDev {
   double* sums;          // [n_req][2][cuts]: sums of exponentials
   double* left;          // [n_req][cuts]: sums of what is drawn from
   int32_t* tickets;      // [n_req]
+  int32_t* active;       // [kVSteps][1 + n_req]: requests of the draw's further steps, behind their number
   int32_t* paths;        // [n_rows]
 };
 
@@ -121,7 +131,9 @@ __device__ __forceinline__ bool nodes_of(const mca_verify_drafts_args& a, int r,
 }  // namespace
 
 // Sums of a row's part: grid (rows, parts of the target's, then of the draft's).  Rows
-// of no request, and draft rows of nodes without children, are left out.
+// of no request, and draft rows of nodes without children, are left out.  Bound by the
+// loads: four of 16 bytes a lane in flight, the running maximum kept by each lane so that
+// nothing waits for another before the end.
 template <int TYPE, bool GREEDY>
 __global__ __launch_bounds__(kVThreads) void k_lm_verify_rows(VerifyDev p) {
   constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
@@ -305,8 +317,7 @@ __device__ __forceinline__ End walk(const VerifyDev& d, int r, int first, int n,
   const int up0 = lane < n ? s.up[lane] : -1, up1 = lane + 64 < n ? s.up[lane + 64] : -1;
   const bool legal0 = lane < n && s.tok[lane] >= 0 && s.tok[lane] < V;
   const bool legal1 = lane + 64 < n && s.tok[lane + 64] >= 0 && s.tok[lane + 64] < V;
-  int node = 0, count = 1, gone = 0;
-  double c = 0;
+  int node = 0, count = 1, gone = 0, lost = 0;
   bool ok = true;
   if (tid == 0) d.paths[first] = first;
   while (true) {
@@ -317,9 +328,8 @@ __device__ __forceinline__ End walk(const VerifyDev& d, int r, int first, int n,
     kids[0] &= __ballot(legal0);
     kids[1] &= __ballot(legal1);
     int go = -1;
-    double sum = 1;
-    c = 0;
-    gone = 0;
+    double sum = 1, c = 0;
+    gone = lost = 0;
     while (true) {
       const int i = kids[0] ? __builtin_ctzll(kids[0]) : (kids[1] ? 64 + __builtin_ctzll(kids[1]) : -1);
       if (i < 0) break;
@@ -335,6 +345,7 @@ __device__ __forceinline__ End walk(const VerifyDev& d, int r, int first, int n,
           break;
         }
         c += sum;
+        ++lost;
         if (kids[0] | kids[1]) sum = left_sum<TYPE, THREADS>(a, first, node, c, s);
       } else {
         // a symbol that was rejected before has nothing left
@@ -358,7 +369,7 @@ __device__ __forceinline__ End walk(const VerifyDev& d, int r, int first, int n,
     a.new_len[r] = a.lengths[r] + count;
     if (GREEDY || !ok) a.token[r] = ok ? s.best[node] : -1;
   }
-  return {ok && !GREEDY ? first + (int64_t)node : -1, c, s.m[0][node], drawn ? s.m[1][node] : 0.f, first, node, gone, 0};
+  return {ok && !GREEDY ? first + (int64_t)node : -1, lost > 0 ? 1.0 : 0.0, s.m[0][node], drawn ? s.m[1][node] : 0.f, first, node, gone, max(lost - 1, 0)};
 }
 // of a request that has no nodes, or too many
 __device__ __forceinline__ void no_walk(const mca_verify_drafts_args& a, int r) {
@@ -516,7 +527,10 @@ __device__ __forceinline__ int last_of(int last, int* s_found) {
 
 }  // namespace
 
-// A request's walk over a large vocabulary, from the rows' parts.
+// A request's walk over a large vocabulary, from the rows' parts.  One workgroup, as
+// whether a child is accepted decides which row is read next; a pass for S over 128000
+// symbols at one rejection takes it 8 us (in 16 waves; in 4 it took 15).  Only children
+// behind a rejected one need such a pass.
 template <int TYPE, bool GREEDY>
 __global__ __launch_bounds__(kWalkThreads) void k_lm_verify_walk(VerifyDev d) {
   const mca_verify_drafts_args& a = d.a;
@@ -525,6 +539,7 @@ __global__ __launch_bounds__(kWalkThreads) void k_lm_verify_walk(VerifyDev d) {
   const int tid = threadIdx.x, r = blockIdx.x;
   int first, n;
   if (tid == 0) d.tickets[r] = 0;
+  if (r == 0 && tid < kVSteps) d.active[tid * (1 + a.n_req)] = 0;
   if (!nodes_of(a, r, &first, &n)) {
     if (tid == 0) {
       no_walk(a, r);
@@ -631,20 +646,23 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_compact(VerifyDev d) {
   compact(d, s_wave);
 }
 
-// The draw: every cut's sum of what is drawn from; the request's last workgroup finds
-// the cut, then the symbol.  Workgroup (n_req, 0) puts the rows together.
+namespace {
+
+struct DrawShared {
+  double red[kVWaves], all[kVMaxSplits];
+  int gone[MCA_MAX_NODES];
+  int last, found;
+};
+
+// A step of the draw for one request and cut: the cut's sum of what is left by c.  The
+// request's last workgroup adds the sums to c while there are more rejections; behind them
+// it finds the cut, then the symbol.  In the last step it goes through further rejections
+// by itself.
 template <int TYPE>
-__global__ __launch_bounds__(kVThreads) void k_lm_verify_draw(VerifyDev d) {
+__device__ __forceinline__ void draw_cut(const VerifyDev& d, int r, int cut, int step, int steps, DrawShared& s) {
   const mca_verify_drafts_args& a = d.a;
-  __shared__ double s_red[kVWaves], s_all[kVMaxSplits];
-  __shared__ int s_wave[kVWaves], s_gone[MCA_MAX_NODES];
-  __shared__ int s_last, s_found;
-  const int tid = threadIdx.x, lane = tid & 63, r = blockIdx.x, cut = blockIdx.y;
-  if (r == a.n_req) {
-    if (cut == 0) compact(d, s_wave);
-    return;
-  }
-  const End e = d.ends[r];
+  const int tid = threadIdx.x, lane = tid & 63;
+  End e = d.ends[r];
   if (e.row < 0) return;
   // (every wave for itself, a cut a lane)
   double sp = 1, sq = 1;
@@ -653,13 +671,14 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_draw(VerifyDev d) {
     sp = wave_sum(lane < d.cuts ? sums[lane] : 0.0);
     sq = wave_sum(lane < d.cuts ? sums[d.cuts + lane] : 0.0);
   }
-  const Weights f = weights_of<TYPE>(a, e, sp, sq, s_gone, gone_symbols(a, e, s_gone, &s_found));
+  Weights f = weights_of<TYPE>(a, e, sp, sq, s.gone, gone_symbols(a, e, s.gone, &s.found));
   int lo, hi;
   cut_of(d, cut, &lo, &hi);
-  // First this cut's sum; then, of the request's last workgroup, the cut in which the goal
-  // lies (and, where nothing is left, between them the sums of p over all cuts).  One body
-  // serves them all: nothing here runs often enough to pay for more instructions.
-  bool plain = false, finding = false;
+  // First this cut's sum; then, of the request's last workgroup, sums over all cuts where
+  // it has to go on alone (more rejections, or nothing is left and p itself is drawn from),
+  // and the cut in which the goal lies.  One body serves them all: nothing here runs often
+  // enough to pay for more instructions.
+  bool plain = false, finding = false, alone = false;
   int x = 0, last = -1;
   double before = 0, goal = 0;
   while (true) {
@@ -670,7 +689,7 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_draw(VerifyDev d) {
       double w[kVSide];
       weigh<TYPE, kVSide>(f, v0, hi, plain, w);
       if (finding) {
-        const int found = past_goal<kVSide>(w, v0, goal, &before, &last, s_red, &s_found);
+        const int found = past_goal<kVSide>(w, v0, goal, &before, &last, s.red, &s.found);
         if (found == 0x7fffffff) continue;
         if (tid == 0) a.token[r] = found;
         return;
@@ -679,34 +698,53 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_draw(VerifyDev d) {
       for (int i = 0; i < kVSide; ++i) mine += w[i];
     }
     if (finding) {
-      const int found = last_of(last, &s_found);
+      const int found = last_of(last, &s.found);
       if (tid == 0) a.token[r] = found;
       return;
     }
-    mine = group_sum<kVWaves>(mine, s_red);
-    if (!plain) {
+    mine = group_sum<kVWaves>(mine, s.red);
+    if (!alone) {
       if (tid == 0) {
         // The sums are written and read past the caches (agent scope), so that the ticket
         // only has to wait for its own: no cache is written back or emptied for it.
         __hip_atomic_store(&d.left[(int64_t)r * d.cuts + cut], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        s_last = __hip_atomic_fetch_add(&d.tickets[r], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == d.cuts - 1;
+        s.last = __hip_atomic_fetch_add(&d.tickets[r], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == d.cuts - 1;
       }
       __syncthreads();
-      if (!s_last) return;
+      if (!s.last) return;
       mine = lane < d.cuts ? __hip_atomic_load(&d.left[(int64_t)r * d.cuts + lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
     } else {
-      if (tid == 0) s_all[x] = mine;
+      if (tid == 0) s.all[x] = mine;
       if (++x < d.cuts) {
         cut_of(d, x, &lo, &hi);
         continue;
       }
       __syncthreads();
-      mine = lane < d.cuts ? s_all[lane] : 0.0;
+      mine = lane < d.cuts ? s.all[lane] : 0.0;
+      __syncthreads();
     }
     const double total = wave_sum(mine);
-    if (!plain && !(total > 0)) {
-      plain = true;
+    if (e.more > 0 || (!plain && !(total > 0))) {
+      if (e.more > 0) {
+        e.c += total;
+        --e.more;
+        if (step < steps - 1) {
+          if (tid == 0) {
+            d.ends[r].c = e.c;
+            d.ends[r].more = e.more;
+            d.tickets[r] = 0;
+            int32_t* list = d.active + (int64_t)step * (1 + a.n_req);
+            list[1 + atomicAdd(list, 1)] = r;
+          }
+          return;
+        }
+        f.iq = e.c / sq;
+      } else {
+        plain = true;
+      }
+      alone = true;
+      x = 0;
       cut_of(d, 0, &lo, &hi);
       continue;
     }
@@ -727,6 +765,36 @@ __global__ __launch_bounds__(kVThreads) void k_lm_verify_draw(VerifyDev d) {
     before = __shfl(run - mine, at, 64);
     cut_of(d, at, &lo, &hi);
     finding = true;
+  }
+}
+
+}  // namespace
+
+// The first step, of all requests and cuts: 13 us from the first workgroup to the last
+// (their weights take 3 to 4, the other 7 pass until the last one has started), 5 for the
+// request's last workgroup to find the symbol.  Workgroup (n_req, 0) puts the rows together.
+template <int TYPE>
+__global__ __launch_bounds__(kVThreads) void k_lm_verify_draw(VerifyDev d, int steps) {
+  __shared__ DrawShared s;
+  __shared__ int s_wave[kVWaves];
+  if ((int)blockIdx.x == d.a.n_req) {
+    if (blockIdx.y == 0) compact(d, s_wave);
+    return;
+  }
+  draw_cut<TYPE>(d, blockIdx.x, blockIdx.y, 0, steps, s);
+}
+
+// Further ones, of the requests that the step before has named, by as many workgroups as
+// run together (with two steps 97 us in the above; where all of them start again, most to end
+// at once, 101).
+template <int TYPE>
+__global__ __launch_bounds__(kVThreads) void k_lm_verify_draw_more(VerifyDev d, int step, int steps) {
+  __shared__ DrawShared s;
+  const int32_t* list = d.active + (int64_t)(step - 1) * (1 + d.a.n_req);
+  const int64_t items = (int64_t)list[0] * d.cuts;
+  for (int64_t x = blockIdx.x; x < items; x += gridDim.x) {
+    draw_cut<TYPE>(d, list[1 + x / d.cuts], (int)(x % d.cuts), step, steps, s);
+    __syncthreads();
   }
 }
 
@@ -821,10 +889,11 @@ __global__ __launch_bounds__(kWalkThreads) void k_lm_verify_whole(VerifyDev d) {
   if (GREEDY || e.row < 0) return;
   double sp = s.sum[0][e.node], sq = s.sum[1][e.node];
   if (e.c != 0 && !exact) exp_sums<TYPE, EACH, THREADS>(weights_of<TYPE>(a, e, 1, 1, nullptr, 0), 0, V, s.red, &sp, &sq);
-  const Weights f = weights_of<TYPE>(a, e, sp, sq, s_gone, gone_symbols(a, e, s_gone, &s_count));
+  Weights f = weights_of<TYPE>(a, e, sp, sq, s_gone, gone_symbols(a, e, s_gone, &s_count));
   const int segments = (V + kVSegment - 1) / kVSegment;
-#pragma unroll 1
-  for (int plain = 0; plain < 2; ++plain) {  // 1: nothing is left, from p itself
+  int more = e.more, plain = 0;  // rejections to be added to c; nothing is left, from p itself
+  double c = e.c;
+  while (true) {
 #pragma unroll 1
     for (int x = wave; x < segments; x += WAVES) {
       double w[EACH];
@@ -844,7 +913,14 @@ __global__ __launch_bounds__(kWalkThreads) void k_lm_verify_whole(VerifyDev d) {
       if (lane >= y) run += up;
     }
     const double total = __shfl(run, 63, 64);
-    if (!(total > 0) && plain == 0) {
+    if (more > 0 || (!(total > 0) && plain == 0)) {
+      if (more > 0) {
+        c += total;
+        --more;
+        f.iq = c / sq;
+      } else {
+        plain = 1;
+      }
       __syncthreads();
       continue;
     }
@@ -889,14 +965,21 @@ __global__ __launch_bounds__(kWalkThreads) void k_lm_verify_whole(VerifyDev d) {
 
 namespace {
 
+// Parts of a row in the first step: enough for 2048 workgroups, of 8192 symbols or more.
+// (us of the whole call for 512, 2048 and 8192: trees of 9 nodes for 32 requests, 128000 bf16
+// symbols 102.5, 97.2 and 99.7; with parts of 4096 one request of 5 nodes 30.3 for 28.1.)
 int row_splits(const mca_verify_drafts_args& a) {
   const int64_t rows = std::max<int64_t>(1, a.n_rows) * (a.draft != nullptr && !a.greedy ? 2 : 1);
   return (int)std::clamp<int64_t>(std::min((2048 + rows - 1) / rows, a.n_vocab / kVPart), 1, kVMaxSplits);
 }
+// Parts of a row in the draw: enough for four workgroups a compute unit, of 2048 symbols or
+// more.  (Us, bf16, with 256, 512, 1024 and 2048 workgroups: 32 requests of trees, 128000 symbols
+// 133, 107, 100 and 105; 150 chains of 4 drafts, 32000 symbols 87, 70, 68 and 69.  With parts of 4096 symbols
+// and of 2048: one request of 128000 symbols 30.5 and 28.7, 8 of 50000 35.6 and 31.5, 32 of 32000 with four
+// children a node 111 and 116.)
 int end_cuts(const mca_verify_drafts_args& a) {
-  const int64_t reqs = std::max(1, a.n_req);
-  const int64_t cuts = (a.n_vocab + kVCut - 1) / kVCut;
-  return (int)std::clamp<int64_t>(std::min(cuts * (reqs * cuts <= 256 ? 2 : 1), std::max((4096 + reqs - 1) / reqs, (cuts + 3) / 4)), 1, kVMaxSplits);
+  const int64_t reqs = std::max(1, a.n_req), cuts = (a.n_vocab + kVCut - 1) / kVCut;
+  return (int)std::clamp<int64_t>(std::min(cuts, (1024 + reqs - 1) / reqs), 1, kVMaxSplits);
 }
 size_t room(size_t n) { return (n + 255) / 256 * 256; }
 // A request in one workgroup, while its rows are few values in all.  (bf16, 32 requests,
@@ -929,6 +1012,7 @@ size_t lay_out(const mca_verify_drafts_args& a, VerifyDev* d) {
   d->sums = (double*)take((size_t)a.n_req * 2 * cuts * sizeof(double));
   d->left = (double*)take((size_t)a.n_req * cuts * sizeof(double));
   d->tickets = (int32_t*)take((size_t)a.n_req * sizeof(int32_t));
+  d->active = (int32_t*)take((size_t)kVSteps * (1 + a.n_req) * sizeof(int32_t));
   d->paths = (int32_t*)take((size_t)a.n_rows * sizeof(int32_t));
   return n;
 }
@@ -960,7 +1044,13 @@ void launch(const VerifyDev& d, hipStream_t s) {
   if (a.n_rows > 0) hipLaunchKernelGGL((k_lm_verify_rows<TYPE, false>), rows, threads, 0, s, d);
   hipLaunchKernelGGL((k_lm_verify_walk<TYPE, false>), dim3((unsigned)a.n_req), dim3(kWalkThreads), 0, s, d);
   if (both == 2) hipLaunchKernelGGL((k_lm_verify_sums<TYPE>), dim3((unsigned)a.n_req, (unsigned)d.cuts), threads, 0, s, d);
-  hipLaunchKernelGGL((k_lm_verify_draw<TYPE>), dim3((unsigned)a.n_req + 1, (unsigned)d.cuts), threads, 0, s, d);
+  // A node has at most max_nodes - 1 children.  (us with 1, 2 and 3 further steps: 32 requests
+  // of trees of 9 nodes with four children each, 32000 symbols 150, 119 and 86, with two 96.5, 97.3
+  // and 99.8, 128000 symbols; of chains of 5, which need none, 41, 43 and 44.)
+  const int steps = 1 + (both == 2 ? std::clamp(a.max_nodes - 2, 0, kVSteps) : 0);
+  hipLaunchKernelGGL((k_lm_verify_draw<TYPE>), dim3((unsigned)a.n_req + 1, (unsigned)d.cuts), threads, 0, s, d, steps);
+  for (int i = 1; i < steps; ++i)
+    hipLaunchKernelGGL((k_lm_verify_draw_more<TYPE>), dim3((unsigned)std::min<int64_t>(512, (int64_t)a.n_req * d.cuts)), threads, 0, s, d, i, steps);
 }
 
 }  // namespace

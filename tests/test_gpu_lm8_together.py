@@ -189,7 +189,7 @@ def test_a_step_over_the_cache_of_8_bits(lm, typ, captured):
             assert (np.abs(h["att"][row, head] - o) <= tol).all()
         w = olm.verify_drafts(h["logits"], host(draft), host(tokens), host(parents), host(offsets), before["lens"], host(accept),
                               host(sample), 0.8, 1.0, False, R * n)
-        assert w[3] > 2.0 ** -16 and w[4] > 2.0 ** -45
+        assert w[3] > 2.0 ** -16 and w[4] > 2.0 ** -40
         for g, x in zip(got, w):
             np.testing.assert_array_equal(g, x)
         tab, fr, off, _, st = olm.block_tables(before["lens"], w[0], before["table"], before["free"], B, R * n)

@@ -5,7 +5,7 @@ it lies closer to its border than the arithmetic resolves.  Where a child is tri
 are sums of 32-bit exponentials, which are off by (2 + |exponent|) 2^-24 each and by
 another 2^-24 for each of a lane's terms: below 2^-16 of the sum at the sizes here, as
 exponents of more than 30 weigh nothing.  Where a token is drawn they are sums of V 64-bit
-ones, each off by 2^-47: below 2^-45.  The seeds' margins, which the oracle gives, are
+ones, each off by 2^-47, and c is a sum of such sums: below 2^-40.  The seeds' margins, which the oracle gives, are
 asserted to be wider.
 """
 import numpy as np
@@ -59,7 +59,7 @@ def expected(s):
                              h["scale"], h["draft_scale"], h["greedy"], len(h["tokens"]))
 
 
-def check(lm, s, got=None, margins=(2.0 ** -16, 2.0 ** -45)):
+def check(lm, s, got=None, margins=(2.0 ** -16, 2.0 ** -40)):
     want = expected(s)
     assert s["greedy"] or (want[3] > margins[0] and want[4] > margins[1]), want[3:]
     got = lm.mca_verify_drafts(**s) if got is None else got
@@ -80,6 +80,20 @@ def test_verify(lm, typ, mode, vocab, nodes, width):
         want = check(lm, s, margins=(-1, -1)) if vocab == 1 else check(lm, s)
         got += int((want[0] - host(s["lengths"]) > 1).sum())
     assert got > 0 or vocab == 1 or mode == "given"  # a given symbol among 20011 is seldom accepted
+
+
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("mode", ["draft", "given"])
+@pytest.mark.parametrize("vocab", [400, 9000, 40001])
+def test_many_rejections_at_a_node(lm, typ, mode, vocab):
+    """One to nine children, all or nearly all of which are rejected: the token is drawn from what all of them leave."""
+    lost = 0
+    for kids in (1, 2, 3, 4, 5, 9):
+        s = make(kids, typ, [kids + 1] * 8, vocab, kids, mode, noise=0.4)
+        s["accept"].uniform_(0.9, 1.0, generator=torch.Generator("cuda").manual_seed(kids))
+        want = check(lm, s)
+        lost += int((want[0] - host(s["lengths"]) == 1).sum())
+    assert lost > 6
 
 
 @pytest.mark.parametrize("pad", [1, 3, 8])

@@ -7,8 +7,12 @@
 // the largest of those, and the teacher's are added behind the pass: the loss takes the
 // logarithm of the first, which a difference of nearly equal sums, or exponentials relative
 // to the largest logit of all, would lose where the teacher's symbols have nearly all
-// weight.  Which of a row's 16-byte vectors hold a teacher's symbol is a bit each in
-// LDS, so that the entries are compared only with those vectors' values.
+// weight.
+//
+// Bound by the logits' bytes for large vocabularies: bf16, 4096 rows of 50001 symbols, 20
+// entries and rest, are 79 us (410 MB, 5.2 TB/s) and with the gradient 148 more (820 MB read and
+// written, 5.5 TB/s); a large copy reaches 5.1 TB/s on this card.  For small ones by the entries'
+// 64-bit chains of a wave: 8192 rows of 65, 7.5 and 7.0 us (2.2 MB read, as much written).
 #include <algorithm>
 
 #include "device_common.hpp"
@@ -23,6 +27,7 @@ constexpr int kDsThreads = 256;
 constexpr int kDsWaves = kDsThreads / 64;
 constexpr int kDsUnroll = 4;
 constexpr int kDsSmall = 1024;     // largest vocabulary of the wave-per-row kernels
+constexpr int64_t kDsFew = 1024;   // rows up to which that is kDsSmall / 2
 constexpr int kDsSplits = 64;      // most parts of a row
 constexpr int64_t kDsPart = 8192;  // symbols of a part at least
 constexpr float kLowest = -3.402823466e38f;
@@ -186,8 +191,10 @@ __device__ __forceinline__ void finish(const mca_distill_args& p, int64_t t, con
 
 }  // namespace
 
-// Rows of more than kDsSmall symbols: a workgroup per row, or per part of one (grid y),
-// in one pass of its first four waves; the fifth has the row's entries meanwhile.
+// Larger rows: a workgroup per row, or per part of one (grid y), in one pass of its first
+// four waves; the fifth has the row's entries meanwhile (behind the pass they cost 15 us of the
+// 79).  With `rest` the teacher's symbols leave the pass in the registers: a ballot finds those
+// among a round's 8192 bytes, mostly none (compared with each vector, they cost 40 us).
 template <int TYPE>
 __global__ __launch_bounds__(kDsThreads + 64) void k_lm_distill(mca_distill_args p, int splits, Sums* parts) {
   constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
@@ -288,7 +295,9 @@ __global__ __launch_bounds__(64) void k_lm_distill_join(mca_distill_args p, int 
   finish(p, t, known_of<TYPE>(p, t, entry_of(p, t, lane)), m, wave_sum(f * x.s));
 }
 
-// Rows of at most 64 N symbols: a wave per row, the row in registers.
+// Rows of at most 64 N symbols: a wave per row, the row in registers.  Bound by the
+// entries' chain (an exponential, two logarithms of 64 bits and the sums over lanes), which
+// waves of other rows fill.
 template <int TYPE, int N>
 __global__ __launch_bounds__(kDsThreads) void k_lm_distill_small(mca_distill_args p) {
   typedef typename Elem<TYPE>::Raw Raw;
@@ -360,7 +369,9 @@ __device__ __forceinline__ float prob(float z, float scale, float lse) {
 
 }  // namespace
 
-// Long rows: a workgroup takes 256 x kDsUnroll vectors of one row.
+// Long rows: a workgroup takes 256 x kDsUnroll vectors of one row.  Which of them hold a
+// teacher's symbol is a bit each in LDS, so that the entries are compared only with those
+// vectors' values.
 template <int TYPE>
 __global__ __launch_bounds__(kDsThreads) void k_lm_distill_grad(mca_distill_grad_args p) {
   constexpr int VE = Elem<TYPE>::kPer, EL = Elem<TYPE>::kSize;
@@ -478,10 +489,15 @@ __global__ __launch_bounds__(kDsThreads) void k_lm_distill_grad_rows(mca_distill
   }
 }
 
+// Rows of more than 65536 symbols are split while they are fewer than 512.  (us whole and
+// split, bf16: one row of 128000 12.2 and 7.4, 64 rows 15.7 and 10.6, 128 of them in fp32 22.5 and
+// 16.9; but 300 rows 20.6 and 20.9, and of 50000 symbols one to 16 rows 7.7 and 8.1, 128 9.3 and 10.4:
+// the second launch costs more than the first one's pass.  For 1024 workgroups and more, 600
+// rows of 128000 take 36.6 for 32.6.)
 LogprobsPlan lm_distill_plan(const mca_distill_args& a) {
   LogprobsPlan p{1, 0};
-  if (a.n_vocab <= 2 * kDsPart || a.n_rows == 0) return p;
-  const int64_t want = (1024 + a.n_rows - 1) / a.n_rows, most = (a.n_vocab + kDsPart - 1) / kDsPart;
+  if (a.n_vocab <= 8 * kDsPart || a.n_rows == 0) return p;
+  const int64_t want = (512 + a.n_rows - 1) / a.n_rows, most = (a.n_vocab + kDsPart - 1) / kDsPart;
   p.splits = (int32_t)std::clamp<int64_t>(std::min(want, most), 1, kDsSplits);
   if (p.splits > 1) p.bytes = (size_t)a.n_rows * p.splits * sizeof(Sums);
   return p;
@@ -489,6 +505,9 @@ LogprobsPlan lm_distill_plan(const mca_distill_args& a) {
 
 namespace {
 
+// A wave per row up to kDsSmall symbols, of few rows up to half of that.  (us of a wave and of
+// a workgroup a row, bf16: 4096 rows of 512 symbols 7.3 and 15.3, of 1000 11.6 and 15.4; 1024 rows
+// of 512 5.9 and 5.8, of 1000 6.9 and 5.8; 16 rows of 300 5.5 and 5.7, of 1000 6.7 and 5.2.)
 template <int TYPE>
 void launch_distill(const mca_distill_args& a, const LogprobsPlan& plan, hipStream_t s) {
   const dim3 threads(kDsThreads), grid((unsigned)((a.n_rows + kDsWaves - 1) / kDsWaves));
@@ -498,7 +517,7 @@ void launch_distill(const mca_distill_args& a, const LogprobsPlan& plan, hipStre
     hipLaunchKernelGGL((k_lm_distill_small<TYPE, 4>), grid, threads, 0, s, a);
   else if (a.n_vocab <= 512)
     hipLaunchKernelGGL((k_lm_distill_small<TYPE, 8>), grid, threads, 0, s, a);
-  else if (a.n_vocab <= kDsSmall)
+  else if (a.n_vocab <= kDsSmall && a.n_rows > kDsFew)
     hipLaunchKernelGGL((k_lm_distill_small<TYPE, 16>), grid, threads, 0, s, a);
   else {
     Sums* parts = (Sums*)a.workspace;
@@ -508,12 +527,15 @@ void launch_distill(const mca_distill_args& a, const LogprobsPlan& plan, hipStre
   }
 }
 
+// Vectors from 768 symbols on, where logits and gradient allow.  (us of a wave a row, value
+// by value, and of vectors, bf16: 4096 rows of 512 symbols 6.4 and 9.0, of 700 8.8 and 11.4, of 1000
+// 11.4 and 10.5, of 2000 18.9 and 12.6; 16 rows of 300 4.5 and 5.6, of 1000 6.6 and 4.7.)
 template <int TYPE>
 void launch_distill_grad(const mca_distill_grad_args& a, hipStream_t s) {
   const int el = Elem<TYPE>::kSize;
   const bool alike = (((uintptr_t)a.logits - (uintptr_t)a.grad) & 15) == 0 &&
                      (((a.logits_row - a.grad_row) * el) & 15) == 0;
-  if (a.n_vocab >= 512 && alike) {
+  if (a.n_vocab >= 768 && alike) {
     const int64_t per = (int64_t)kDsThreads * kDsUnroll * Elem<TYPE>::kPer;
     for (int64_t t0 = 0; t0 < a.n_rows; t0 += 65535) {  // grid y
       mca_distill_grad_args b = a;

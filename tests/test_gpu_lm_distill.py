@@ -146,6 +146,20 @@ def test_masked_and_undefined(lm, typ, vocab, rest):
     check(lm, s)
 
 
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("rows,vocab,top,rest", [(1030, 513, 5, True), (1101, 1000, 20, False), (1024, 767, 3, True), (3, 65537, 20, True), (5, 100003, 32, True)])
+def test_where_the_kernels_change(lm, typ, rows, vocab, top, rest):
+    """Short rows while they are many, and long ones in parts while they are few."""
+    check(lm, make(rows, typ, rows, vocab, top, rest))
+
+
+@pytest.mark.parametrize("typ", TYPES)
+def test_rows_in_parts(lm, typ):
+    test_symbols_that_are_none_and_twice(lm, 70000, True)
+    test_masked_and_undefined(lm, typ, 70000, True)
+    test_masked_and_undefined(lm, typ, 70000, False)
+
+
 def test_the_teachers_symbols_have_nearly_all_weight(lm):
     """The others' probability is 1e-12 and less: its logarithm is as exact as ever."""
     for vocab in (90, 5000, 40000):

@@ -435,7 +435,8 @@ def mca_verify_drafts(target, draft, tokens, parents, offsets, lengths, max_node
         _flat(dev, f32, "accept", accept, n)
         _flat(dev, f32, "sample", sample, n_req)
         a.accept, a.sample = accept.data_ptr(), sample.data_ptr()
-    new_len, token = torch.empty((2, n_req), dtype=i32, device=dev).unbind()
+    # (tensors of their own: parts of one cost three times as much host time)
+    new_len, token = torch.empty(n_req, dtype=i32, device=dev), torch.empty(n_req, dtype=i32, device=dev)
     rows = torch.empty(n, dtype=i32, device=dev)
     a.new_len, a.token, a.rows = new_len.data_ptr(), token.data_ptr(), rows.data_ptr()
     lib = load_library()
@@ -595,9 +596,8 @@ def mca_distill(logits, logprob, ids, rest: bool = False, scale: float = 1.0, wo
     a = mca_distill_args()
     _teacher(a, dev, logits, logprob, ids, rest, scale)
     n = a.n_rows
-    loss, lse, lse_rest = torch.empty((3, n), dtype=f32, device=dev).unbind()
-    if not rest:
-        lse_rest = lse_rest[:0]
+    loss, lse = torch.empty(n, dtype=f32, device=dev), torch.empty(n, dtype=f32, device=dev)
+    lse_rest = torch.empty(n if rest else 0, dtype=f32, device=dev)
     a.loss, a.lse = loss.data_ptr(), lse.data_ptr()
     if rest:
         a.lse_rest = lse_rest.data_ptr()

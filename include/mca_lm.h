@@ -244,7 +244,7 @@ int mca_tree_attention8(const mca_tree_attention8_args* args, void* hip_stream);
 typedef struct mca_verify_drafts_args {
   int32_t dtype, n_req, max_nodes, greedy;
   int64_t n_rows, n_vocab, target_row, draft_row;
-  double scale, draft_scale;
+  double scale, draft_scale; /* 2^-100 to 2^100 */
   const void* target;
   const void* draft;      /* or NULL */
   const int32_t* tokens;  /* [n_rows] */
@@ -326,7 +326,7 @@ int mca_token_logprobs_grad(const mca_token_logprobs_grad_args* args, void* hip_
  * entries, whose q add up (each with a term of its own). */
 typedef struct mca_distill_args {
   int32_t dtype, n_top, rest;
-  float scale; /* positive */
+  float scale; /* 2^-100 to 2^100 */
   int64_t n_rows, n_vocab, logits_row;
   const void* logits;
   const float* logprob; /* [n_rows][n_top] */

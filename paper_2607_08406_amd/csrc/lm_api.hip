@@ -82,6 +82,10 @@ const char* check_cache8(int32_t n_req, int32_t n_kv_head, int32_t head_dim, int
   return nullptr;
 }
 
+// Temperatures that multiply logits in 32 bits: neither they nor their product with log2 e
+// overflow or vanish, which would make NaN of 0 or -inf.
+bool scale_ok(double x) { return x >= 0x1p-100 && x <= 0x1p100; }
+
 const char* check_verify(const mca_verify_drafts_args& a, int* code) {
   *code = MCA_EINVAL;
   if (!known_type(a.dtype)) return "unknown dtype";
@@ -102,7 +106,7 @@ const char* check_distill(int32_t dtype, int32_t n_top, int32_t rest, float scal
   if (n_rows < 0) return "n_rows must not be negative";
   if (n_vocab < 1) return "n_vocab must be positive";
   if (n_top < 1 || n_top > MCA_MAX_TOP) return "n_top out of range [1, 32]";
-  if (!std::isfinite(scale) || !(scale > 0)) return "scale must be positive and finite";
+  if (!scale_ok(scale)) return "scale must be positive, from 2^-100 to 2^100";
   if (rest != 0 && rest != 1) return "rest must be 0 or 1";
   if (rest == 1 && scale != 1.0f) return "the other symbols as one outcome (rest) take a scale of 1";
   *code = MCA_EUNSUPPORTED;
@@ -361,8 +365,8 @@ int mca_verify_drafts(const mca_verify_drafts_args* args, void* hip_stream) {
   if (msg != nullptr) return mca::lm_fail(code, msg);
   if (a.greedy != 0 && a.greedy != 1) return invalid("greedy must be 0 or 1");
   const bool draft = a.draft != nullptr && !a.greedy;
-  if (!a.greedy && (!std::isfinite(a.scale) || !(a.scale > 0))) return invalid("scale must be positive and finite");
-  if (draft && (!std::isfinite(a.draft_scale) || !(a.draft_scale > 0))) return invalid("draft_scale must be positive and finite");
+  if (!a.greedy && !scale_ok(a.scale)) return invalid("scale must be positive, from 2^-100 to 2^100");
+  if (draft && !scale_ok(a.draft_scale)) return invalid("draft_scale must be positive, from 2^-100 to 2^100");
   if (a.target_row < a.n_vocab || a.target_row > kMaxStride) return invalid("target_row must be at least n_vocab");
   if (draft && (a.draft_row < a.n_vocab || a.draft_row > kMaxStride)) return invalid("draft_row must be at least n_vocab");
   if (a.n_req == 0 && a.n_rows == 0) return MCA_OK;

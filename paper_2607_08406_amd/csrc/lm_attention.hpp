@@ -589,6 +589,9 @@ __device__ __forceinline__ bool share_begin(const AttnDev& p, int (&s_wave)[NW],
 // requests of 1000 to 2000, one row a head, 4 key heads of 128, bf16: 0.6 GB in
 // 131 us).  Small calls are bound by the chain of table entry, K, scores, V (64 drafts
 // of up to 8 nodes over at most 120 tokens, 4 heads of 32, fp32: 8.5 us).
+// Over codes the same; a code's conversion and scale are one instruction for two, which
+// memory still hides: 32 single tokens behind 8192 to 32768, 8 key heads of 128, 4 rows a
+// head, bf16 (1.33 GB): 250 us and 10 of joining, 5.3 TB/s; the drafts of 8 8.1 us.
 
 // Waves of a SIMD that its registers are for, of 8-bit caches; of shared work few enough
 // that nothing of the loop around the items goes to scratch memory.
@@ -853,6 +856,8 @@ __global__ __launch_bounds__(kAttnThreads, C8 ? resident8(TYPE, DP, SHARE) : 1) 
 // product reaches; of 16384, 512 rows, 8 key heads, bf16 830 and fp16 800.  One request of 262144, 96 rows,
 // 2 key heads of 64, bf16 (134 MB): 41 and 10.  16 rows of a wave, 32 requests of 8192
 // to 32768, one row a head, 8 key heads of 128, bf16 (2.63 GB): 465 and 8, 5.6 TB/s.
+// Codes are widened once, on their way into LDS, so that the products are the same: the
+// drafts above over them 220 to 244 us and 26 of joining.
 template <int TYPE, int DP, int QT, int NW, bool PAD, bool C8>
 __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 ? 1 : 2) void k_lm_attn_wide(AttnDev) {
   constexpr int EL = TYPE == MCA_TYPE_F32 ? 4 : 2;

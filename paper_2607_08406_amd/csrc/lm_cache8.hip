@@ -5,6 +5,11 @@
 // is one conversion from its value and back, a larger scale changes kept codes only
 // where they become subnormal, and neither the order nor the pieces in which a
 // block's tokens arrive change anything else.
+//
+// Both are bound by memory, and of few tokens by a chain of loads (offsets, the block's
+// number, its scale, the rows): bf16, 8 heads of 128, 65000 rows of 32 requests'
+// prompts are 85 us (266 MB read, 133 written, 4.7 TB/s), the values of 50000 tokens 72 us
+// (102 MB read, 205 written, 4.3 TB/s); 64 requests of 8 rows, 4 heads of 32 fp32, 5.0 and 4.7 us.
 #include <algorithm>
 
 #include "device_common.hpp"
@@ -122,7 +127,9 @@ __device__ __forceinline__ uint32_t recoded(uint32_t codes, float by) {
 
 // W waves take one page of a request and one key head: largest values of K and V
 // first, from all their new rows, then codes.  What fits kC8Loads loads of a lane (64
-// rows of 128, 16-bit, of 4 waves) stays in registers between the two.
+// rows of 128, 16-bit, of 4 waves) stays in registers between the two, so that each row
+// is read once; only pages of more are read again, from the last part to the first, of
+// which the caches still hold the end.
 template <int TYPE, int W>
 __global__ __launch_bounds__(kC8Threads) void k_lm_append8(mca_cache8_append_args a, int64_t units) {
   constexpr int EL = TYPE == MCA_TYPE_F32 ? 4 : 2, VE = 16 / EL, T = 64 * W;
@@ -281,7 +288,10 @@ __global__ __launch_bounds__(kC8Threads) void k_lm_read8(mca_cache8_read_args a,
 
 namespace {
 
-// Waves of a page and head: one while a page's new rows are few.
+// Waves of a page and head: one while a page's new rows are few.  (us with one and four,
+// bf16: 32 requests of 8 rows, 8 heads of 128, 5.8 and 6.5, of 16 6.8 and 7.7, of 32 10.6 and 8.2;
+// 64 rows of 32 7.0 and 7.6, of 64 10.7 and 8.4; the 65000 rows above 109 and 85; read back 200
+// tokens of 64 fp32 8.8 and 7.6, 8 of 32 4.7 and 5.7, 50000 of 128 72 and 72.)
 template <class Args>
 bool four_waves(const Args& a) {
   const int64_t tokens = std::min<int64_t>(a.block_size, (a.n + a.n_req - 1) / a.n_req);

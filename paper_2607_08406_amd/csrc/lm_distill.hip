@@ -521,7 +521,18 @@ void launch_distill(const mca_distill_args& a, const LogprobsPlan& plan, hipStre
     hipLaunchKernelGGL((k_lm_distill_small<TYPE, 16>), grid, threads, 0, s, a);
   else {
     Sums* parts = (Sums*)a.workspace;
-    hipLaunchKernelGGL((k_lm_distill<TYPE>), dim3((unsigned)a.n_rows, (unsigned)plan.splits), dim3(kDsThreads + 64), 0, s, a, plan.splits, parts);
+    constexpr int64_t kMost = 1 << 23;  // rows of a launch: a grid has less than 2^32 threads in x (rows in parts are few)
+    for (int64_t t0 = 0; t0 < a.n_rows; t0 += kMost) {
+      mca_distill_args b = a;
+      b.n_rows = std::min(kMost, a.n_rows - t0);
+      b.logits = (const char*)a.logits + t0 * a.logits_row * Elem<TYPE>::kSize;
+      b.logprob += t0 * a.n_top;
+      b.ids += t0 * a.n_top;
+      b.loss += t0;
+      b.lse += t0;
+      if (b.lse_rest != nullptr) b.lse_rest += t0;
+      hipLaunchKernelGGL((k_lm_distill<TYPE>), dim3((unsigned)b.n_rows, (unsigned)plan.splits), dim3(kDsThreads + 64), 0, s, b, plan.splits, parts);
+    }
     if (plan.splits > 1)
       hipLaunchKernelGGL((k_lm_distill_join<TYPE>), dim3((unsigned)a.n_rows), dim3(64), 0, s, a, plan.splits, parts);
   }

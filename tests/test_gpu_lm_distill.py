@@ -250,3 +250,33 @@ def test_many_rows(lm):
     q = torch.softmax(s["logprob"].double(), 1)
     want = torch.softmax(z, 1).scatter_add(1, s["ids"].long(), -q)
     assert ((grad.double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-6).all()
+
+
+def test_many_longer_rows(lm):
+    """The same of the kernels that take a row by vectors."""
+    s = make(11, "bf16", 66000, 1032, 2, True, size=1.0)
+    z = s["logits"].double()
+    got = lm.mca_distill(**s)
+    assert (got.lse.double() - torch.logsumexp(z, 1)).abs().max() < 1e-5
+    g = torch.ones(66000, device="cuda")
+    grad = lm.mca_distill_grad(s["logits"], s["logprob"], s["ids"], got.lse, got.lse_rest, g, True)
+    q, p, ids = s["logprob"].double().exp(), torch.softmax(z, 1), s["ids"].long()
+    other = (1 - q.sum(1, keepdim=True)).clamp(min=0)
+    rest = 1 - p.gather(1, ids).sum(1, keepdim=True)
+    want = (p - other * p / rest).scatter(1, ids, p.gather(1, ids) - q)
+    assert ((grad.double() - want).abs() <= 2.0 ** -8 * want.abs() + 1e-6).all()
+
+
+def test_more_rows_than_threads_of_a_grid(lm):
+    """2^32 / 320 rows and some."""
+    n, v = 13_421_773 + 5, 1025
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("28 GB of logits")
+    z = torch.zeros(n, v, device="cuda", dtype=torch.bfloat16)
+    z[-1, 3] = z[1 << 23, 3] = 2.0
+    logp, ids = torch.zeros(n, 1, device="cuda"), torch.full((n, 1), 3, device="cuda", dtype=torch.int32)
+    got = lm.mca_distill(z, logp, ids)
+    few = lm.mca_distill(z[-2:], logp[-2:], ids[-2:])
+    at = torch.tensor([0, (1 << 23) - 1, 1 << 23, (1 << 23) + 1, n - 2, n - 1], device="cuda")
+    assert torch.equal(got.loss[at], few.loss[torch.tensor([0, 0, 1, 0, 0, 1], device="cuda")])
+    assert int((got.loss != few.loss[0]).sum()) == 2 and int((got.lse != few.lse[0]).sum()) == 2

@@ -111,6 +111,8 @@ VERIFY = dict(dtype=0, n_req=3, max_nodes=5, greedy=0, n_rows=12, n_vocab=100, t
     (dict(scale=0.0), mca.MCA_EINVAL, "scale"),
     (dict(scale=float("nan")), mca.MCA_EINVAL, "scale"),
     (dict(draft_scale=-1.0), mca.MCA_EINVAL, "draft_scale"),
+    (dict(scale=1e31), mca.MCA_EINVAL, "scale"),
+    (dict(draft_scale=1e-31), mca.MCA_EINVAL, "draft_scale"),
     (dict(target_row=99), mca.MCA_EINVAL, "target_row"),
     (dict(draft_row=99), mca.MCA_EINVAL, "draft_row"),
     (dict(accept=None), mca.MCA_EINVAL, "NULL"),
@@ -134,6 +136,8 @@ BOTH = [
     (dict(n_top=0), mca.MCA_EINVAL, "n_top"),
     (dict(n_top=33), mca.MCA_EINVAL, "n_top"),
     (dict(rest=0, scale=0.0), mca.MCA_EINVAL, "scale"),
+    (dict(rest=0, scale=1e-31), mca.MCA_EINVAL, "scale"),
+    (dict(rest=0, scale=1e31), mca.MCA_EINVAL, "scale"),
     (dict(rest=0, scale=float("inf")), mca.MCA_EINVAL, "scale"),
     (dict(scale=0.5), mca.MCA_EINVAL, "rest"),
     (dict(rest=2), mca.MCA_EINVAL, "rest"),

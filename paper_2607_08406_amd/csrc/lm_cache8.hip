@@ -8,9 +8,10 @@
 //
 // Both are bound by memory, and of few tokens by a chain of loads (offsets, the block's
 // number, its scale, the rows): bf16, 8 heads of 128, 65000 rows of 32 requests'
-// prompts are 85 us (266 MB read, 133 written, 4.7 TB/s), the values of 50000 tokens 72 us
+// prompts are 81 us (266 MB read, 133 written, 4.9 TB/s), the values of 50000 tokens 72 us
 // (102 MB read, 205 written, 4.3 TB/s); 64 requests of 8 rows, 4 heads of 32 fp32, 5.0 and 4.7 us.
 #include <algorithm>
+#include <type_traits>
 
 #include "device_common.hpp"
 #include "lm_device.hpp"
@@ -22,8 +23,11 @@ namespace {
 
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kC8Threads = 256;
-constexpr int kC8Waves = kC8Threads / 64;
+// Pages and heads of a workgroup whose waves take one each; W > 1 waves that take one
+// together are a workgroup.
+constexpr int kC8Pages = 4;
+template <int W>
+constexpr int kC8Threads = 64 * (W == 1 ? kC8Pages : W);
 constexpr int kC8Loads = 4;  // 16-byte loads of K and of V that a lane has in flight
 
 // Exponents of scales: the least (below it fp16 values would be no codes' values any
@@ -110,6 +114,32 @@ __device__ __forceinline__ uint32_t codes_of(const float* f, int e, float most) 
   w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
   return nan == 0 ? (uint32_t)w : ((uint32_t)w & ~(nan * 2 + (nan & 0x01010101u))) | nan;
 }
+// the same of finite values that are at most 448 times 2^e: `by` is 2^-e
+__device__ __forceinline__ uint32_t codes_of(const float* f, float by) {
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(f[0] * by, f[1] * by, 0, false);
+  w = __builtin_amdgcn_cvt_pk_fp8_f32(f[2] * by, f[3] * by, w, true);
+  return (uint32_t)w;
+}
+// Largest magnitudes, as numbers' bits without their signs: of 16-bit types of two halves
+// side by side.  Infinities and NaN come out on top.
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+template <int TYPE>
+__device__ __forceinline__ uint32_t larger(uint32_t top, uint32_t x) {
+  if constexpr (TYPE == MCA_TYPE_F32) {
+    return max(top, x & 0x7fffffffu);
+  } else {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top),
+                                                                  __builtin_bit_cast(u16x2, x & 0x7fff7fffu)));
+  }
+}
+// the magnitude in 32 bits (infinities and NaN stay such)
+template <int TYPE>
+__device__ __forceinline__ uint32_t magnitude(uint32_t top) {
+  if constexpr (TYPE == MCA_TYPE_F32) return top;
+  const uint32_t x = max(top & 0xffffu, top >> 16);
+  if constexpr (TYPE == MCA_TYPE_BF16) return x << 16;
+  return __float_as_uint((float)__builtin_bit_cast(_Float16, (uint16_t)x));
+}
 // four kept codes in a scale 2^down times theirs (down <= 0); NaN stays as it is
 __device__ __forceinline__ uint32_t recoded(uint32_t codes, float by) {
   const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(codes, by, false);
@@ -131,12 +161,12 @@ __device__ __forceinline__ uint32_t recoded(uint32_t codes, float by) {
 // is read once; only pages of more are read again, from the last part to the first, of
 // which the caches still hold the end.
 template <int TYPE, int W>
-__global__ __launch_bounds__(kC8Threads) void k_lm_append8(mca_cache8_append_args a, int64_t units) {
+__global__ __launch_bounds__(kC8Threads<W>) void k_lm_append8(mca_cache8_append_args a, int64_t units) {
   constexpr int EL = TYPE == MCA_TYPE_F32 ? 4 : 2, VE = 16 / EL, T = 64 * W;
   typedef Scale<TYPE> S;
-  __shared__ uint32_t s_top[2][kC8Waves];
+  __shared__ uint32_t s_top[2][W];
   const int wave = threadIdx.x >> 6, tid = threadIdx.x % T;
-  const int64_t unit = (int64_t)blockIdx.x * (kC8Waves / W) + wave / W;
+  const int64_t unit = W == 1 ? (int64_t)blockIdx.x * kC8Pages + wave : (int64_t)blockIdx.x;
   Page pg{};
   const bool any = unit < units && page_of(a, a.lengths, unit / a.n_kv_head, &pg) && pg.block >= 0;
   if (!any) return;  // the same for all waves of a unit
@@ -146,56 +176,84 @@ __global__ __launch_bounds__(kC8Threads) void k_lm_append8(mca_cache8_append_arg
   const int keep = max(0, pg.from - pg.start);
   const uint32_t was_k = a.k_scale[at], was_v = a.v_scale[at];
   u32x4 kx[kC8Loads], vx[kC8Loads];
+  const int step_t = T / per, step_part = T - step_t * per;
   auto load = [&](int c) {
+    int t = (c + tid) / per, part = c + tid - t * per;
 #pragma unroll
     for (int u = 0; u < kC8Loads; ++u) {
-      const int e = c + tid + T * u;
       kx[u] = vx[u] = u32x4{0, 0, 0, 0};
-      if (e < all) {
-        const int t = e / per, part = e - t * per;
+      if (t < tokens) {
         const int64_t row = a.rows != nullptr ? (int64_t)a.rows[pg.row0 + t] : pg.row0 + t;
         if (row >= 0 && row < a.n_src) {
           kx[u] = gload((const u32x4*)((const char*)a.k + (row * a.k_row + h * a.k_head) * EL) + part);
           vx[u] = gload((const u32x4*)((const char*)a.v + (row * a.v_row + h * a.v_head) * EL) + part);
         }
       }
-    }
-  };
-  uint32_t top_k = 0, top_v = 0;
-  auto look = [&](u32x4 x, uint32_t* top) {
-    float f[VE];
-    widen<TYPE>(x, f);
-#pragma unroll
-    for (int i = 0; i < VE; ++i) {
-      const uint32_t b = __float_as_uint(f[i]) & 0x7fffffffu;
-      *top = max(*top, finite_bits(b) ? b : 0u);
+      t += step_t;
+      part += step_part;
+      if (part >= per) {
+        part -= per;
+        ++t;
+      }
     }
   };
   const int last = (all - 1) / (T * kC8Loads) * (T * kC8Loads);
+  // the unit's largest of what its lanes found
+  auto join = [&](uint32_t& x, uint32_t& y) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      x = max(x, (uint32_t)__shfl_xor(x, d, 64));
+      y = max(y, (uint32_t)__shfl_xor(y, d, 64));
+    }
+    if constexpr (W > 1) {
+      if ((threadIdx.x & 63) == 0) {
+        s_top[0][wave] = x;
+        s_top[1][wave] = y;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        x = max(x, s_top[0][w]);
+        y = max(y, s_top[1][w]);
+      }
+    }
+  };
+  uint32_t top_k = 0, top_v = 0;
   for (int c = 0; c <= last; c += T * kC8Loads) {
     load(c);
 #pragma unroll
-    for (int u = 0; u < kC8Loads; ++u) {
-      look(kx[u], &top_k);
-      look(vx[u], &top_v);
-    }
-  }
+    for (int u = 0; u < kC8Loads; ++u)
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    top_k = max(top_k, (uint32_t)__shfl_xor(top_k, d, 64));
-    top_v = max(top_v, (uint32_t)__shfl_xor(top_v, d, 64));
+      for (int i = 0; i < 4; ++i) {
+        top_k = larger<TYPE>(top_k, kx[u][i]);
+        top_v = larger<TYPE>(top_v, vx[u][i]);
+      }
   }
-  if constexpr (W > 1) {
-    if ((threadIdx.x & 63) == 0) {
-      s_top[0][wave] = top_k;
-      s_top[1][wave] = top_v;
-    }
-    __syncthreads();
+  top_k = magnitude<TYPE>(top_k);
+  top_v = magnitude<TYPE>(top_v);
+  join(top_k, top_v);
+  const bool finite = finite_bits(top_k) && finite_bits(top_v);
+  if (!finite) {  // the same for all waves of a unit: once more, of finite values alone
+    top_k = top_v = 0;
+    auto look = [&](u32x4 x, uint32_t* top) {
+      float f[VE];
+      widen<TYPE>(x, f);
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-      top_k = max(top_k, s_top[0][w]);
-      top_v = max(top_v, s_top[1][w]);
+      for (int i = 0; i < VE; ++i) {
+        const uint32_t b = __float_as_uint(f[i]) & 0x7fffffffu;
+        *top = max(*top, finite_bits(b) ? b : 0u);
+      }
+    };
+    for (int c = 0; c <= last; c += T * kC8Loads) {
+      if (last > 0) load(c);
+#pragma unroll
+      for (int u = 0; u < kC8Loads; ++u) {
+        look(kx[u], &top_k);
+        look(vx[u], &top_v);
+      }
     }
+    if constexpr (W > 1) __syncthreads();  // s_top is free
+    join(top_k, top_v);
   }
   // 448 is 1.75 times 2^8
   auto exponent = [&](uint32_t top, uint32_t was, int* before) {
@@ -211,26 +269,36 @@ __global__ __launch_bounds__(kC8Threads) void k_lm_append8(mca_cache8_append_arg
   }
   uint8_t* kc = a.k_cache + at * a.block_size * a.head_dim;
   uint8_t* vc = a.v_cache + at * a.block_size * a.head_dim;
-  const float most_k = ek >= S::kFull ? 240.f : 448.f, most_v = ev >= S::kFull ? 240.f : 448.f;
-  for (int c = last; c >= 0; c -= T * kC8Loads) {
-    if (c != last) load(c);
+  auto write = [&](auto plain) {
+    const float most_k = ek >= S::kFull ? 240.f : 448.f, most_v = ev >= S::kFull ? 240.f : 448.f;
+    const float by_k = __builtin_ldexpf(1.f, -ek), by_v = __builtin_ldexpf(1.f, -ev);
+    for (int c = last; c >= 0; c -= T * kC8Loads) {
+      if (c != last) load(c);
 #pragma unroll
-    for (int u = 0; u < kC8Loads; ++u) {
-      const int e = c + tid + T * u;
-      if (e >= all) continue;
-      const int64_t to = (int64_t)(pg.from - pg.start) * a.head_dim + (int64_t)e * VE;
-      float f[VE];
-      auto put = [&](u32x4 x, uint8_t* cache, int ex, float most) {
-        widen<TYPE>(x, f);
-        if constexpr (VE == 4)
-          gstore((uint32_t*)(cache + to), codes_of(f, ex, most));
-        else
-          gstore((u32x2*)(cache + to), u32x2{codes_of(f, ex, most), codes_of(f + 4, ex, most)});
-      };
-      put(kx[u], kc, ek, most_k);
-      put(vx[u], vc, ev, most_v);
+      for (int u = 0; u < kC8Loads; ++u) {
+        const int e = c + tid + T * u;
+        if (e >= all) continue;
+        const int64_t to = (int64_t)(pg.from - pg.start) * a.head_dim + (int64_t)e * VE;
+        auto put = [&](u32x4 x, uint8_t* cache, int ex, float most, float by) {
+          float f[VE];
+          widen<TYPE>(x, f);
+          uint32_t w[VE / 4];
+#pragma unroll
+          for (int i = 0; i < VE / 4; ++i) w[i] = plain ? codes_of(f + 4 * i, by) : codes_of(f + 4 * i, ex, most);
+          if constexpr (VE == 4)
+            gstore((uint32_t*)(cache + to), w[0]);
+          else
+            gstore((u32x2*)(cache + to), u32x2{w[0], w[1]});
+        };
+        put(kx[u], kc, ek, most_k, by_k);
+        put(vx[u], vc, ev, most_v, by_v);
+      }
     }
-  }
+  };
+  if (finite && max(ek, ev) < S::kFull)
+    write(std::true_type());
+  else
+    write(std::false_type());
   if (keep > 0) {
     auto again = [&](uint8_t* cache, int down) {
       if (down >= 0) return;
@@ -250,10 +318,10 @@ __global__ __launch_bounds__(kC8Threads) void k_lm_append8(mca_cache8_append_arg
 // W waves take one page of a request and one key head: VE codes of K and of V a lane
 // and round, their values to the request's rows.
 template <int TYPE, int W>
-__global__ __launch_bounds__(kC8Threads) void k_lm_read8(mca_cache8_read_args a, int64_t units) {
+__global__ __launch_bounds__(kC8Threads<W>) void k_lm_read8(mca_cache8_read_args a, int64_t units) {
   constexpr int EL = TYPE == MCA_TYPE_F32 ? 4 : 2, VE = 16 / EL, CW = VE / 4, T = 64 * W;
   const int wave = threadIdx.x >> 6, tid = threadIdx.x % T;
-  const int64_t unit = (int64_t)blockIdx.x * (kC8Waves / W) + wave / W;
+  const int64_t unit = W == 1 ? (int64_t)blockIdx.x * kC8Pages + wave : (int64_t)blockIdx.x;
   Page pg{};
   if (unit >= units || !page_of(a, a.start, unit / a.n_kv_head, &pg)) return;
   const int h = (int)(unit % a.n_kv_head);
@@ -288,42 +356,51 @@ __global__ __launch_bounds__(kC8Threads) void k_lm_read8(mca_cache8_read_args a,
 
 namespace {
 
-// Waves of a page and head: one while a page's new rows are few.  (us with one and four,
-// bf16: 32 requests of 8 rows, 8 heads of 128, 5.8 and 6.5, of 16 6.8 and 7.7, of 32 10.6 and 8.2;
-// 64 rows of 32 7.0 and 7.6, of 64 10.7 and 8.4; the 65000 rows above 109 and 85; read back 200
-// tokens of 64 fp32 8.8 and 7.6, 8 of 32 4.7 and 5.7, 50000 of 128 72 and 72.)
+// Waves of a page and head: one while its loads in flight are all of a page's new rows, else
+// four.  (us with one and four, 8 heads, bf16: 32 requests of 8 rows of 128 5.8 and 6.5, of 24 7.8
+// and 5.9, of 40 10.2 and 6.1; the 65000 rows above in blocks of 64 101 and 80, of 32 85 and 79, of 16
+// 77 and 100, of 256 141 and 107; read back 50000 tokens of blocks of 64 73 and 72, of 32 70 and 71, of
+// 16 68 and 84; 120 of 4 heads of 32 fp32 4.7 and 6.3.)
 template <class Args>
-bool four_waves(const Args& a) {
+int waves_of(const Args& a) {
   const int64_t tokens = std::min<int64_t>(a.block_size, (a.n + a.n_req - 1) / a.n_req);
-  return tokens * a.head_dim >= 2048;
+  return tokens * a.head_dim / (a.dtype == MCA_TYPE_F32 ? 4 : 8) <= 64 * kC8Loads ? 1 : 4;
+}
+template <int TYPE>
+void append(const mca_cache8_append_args& a, int waves, int64_t units, dim3 grid, hipStream_t s) {
+  if (waves == 1)
+    hipLaunchKernelGGL((k_lm_append8<TYPE, 1>), grid, dim3(kC8Threads<1>), 0, s, a, units);
+  else
+    hipLaunchKernelGGL((k_lm_append8<TYPE, 4>), grid, dim3(kC8Threads<4>), 0, s, a, units);
+}
+template <int TYPE>
+void read(const mca_cache8_read_args& a, int waves, int64_t units, dim3 grid, hipStream_t s) {
+  if (waves == 1)
+    hipLaunchKernelGGL((k_lm_read8<TYPE, 1>), grid, dim3(kC8Threads<1>), 0, s, a, units);
+  else
+    hipLaunchKernelGGL((k_lm_read8<TYPE, 4>), grid, dim3(kC8Threads<4>), 0, s, a, units);
+}
+template <class Args, class F32, class BF16, class F16>
+hipError_t launch(const Args& a, hipStream_t s, F32 f32, BF16 bf16, F16 f16) {
+  const int64_t units = (a.n / a.block_size + 2 * (int64_t)a.n_req) * a.n_kv_head;
+  const int waves = waves_of(a), each = waves == 1 ? kC8Pages : 1;
+  const dim3 grid((unsigned)((units + each - 1) / each));
+  switch (a.dtype) {
+    case MCA_TYPE_F32: f32(a, waves, units, grid, s); break;
+    case MCA_TYPE_BF16: bf16(a, waves, units, grid, s); break;
+    default: f16(a, waves, units, grid, s); break;
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t lm_launch_append8(const mca_cache8_append_args& a, hipStream_t s) {
-  const int64_t units = (a.n / a.block_size + 2 * (int64_t)a.n_req) * a.n_kv_head;
-  const bool four = four_waves(a);
-  const dim3 grid((unsigned)(four ? units : (units + kC8Waves - 1) / kC8Waves)), threads(kC8Threads);
-  auto go = [&](auto one, auto more) { hipLaunchKernelGGL(four ? more : one, grid, threads, 0, s, a, units); };
-  switch (a.dtype) {
-    case MCA_TYPE_F32: go(k_lm_append8<MCA_TYPE_F32, 1>, k_lm_append8<MCA_TYPE_F32, kC8Waves>); break;
-    case MCA_TYPE_BF16: go(k_lm_append8<MCA_TYPE_BF16, 1>, k_lm_append8<MCA_TYPE_BF16, kC8Waves>); break;
-    default: go(k_lm_append8<MCA_TYPE_F16, 1>, k_lm_append8<MCA_TYPE_F16, kC8Waves>); break;
-  }
-  return hipGetLastError();
+  return launch(a, s, append<MCA_TYPE_F32>, append<MCA_TYPE_BF16>, append<MCA_TYPE_F16>);
 }
 
 hipError_t lm_launch_read8(const mca_cache8_read_args& a, hipStream_t s) {
-  const int64_t units = (a.n / a.block_size + 2 * (int64_t)a.n_req) * a.n_kv_head;
-  const bool four = four_waves(a);
-  const dim3 grid((unsigned)(four ? units : (units + kC8Waves - 1) / kC8Waves)), threads(kC8Threads);
-  auto go = [&](auto one, auto more) { hipLaunchKernelGGL(four ? more : one, grid, threads, 0, s, a, units); };
-  switch (a.dtype) {
-    case MCA_TYPE_F32: go(k_lm_read8<MCA_TYPE_F32, 1>, k_lm_read8<MCA_TYPE_F32, kC8Waves>); break;
-    case MCA_TYPE_BF16: go(k_lm_read8<MCA_TYPE_BF16, 1>, k_lm_read8<MCA_TYPE_BF16, kC8Waves>); break;
-    default: go(k_lm_read8<MCA_TYPE_F16, 1>, k_lm_read8<MCA_TYPE_F16, kC8Waves>); break;
-  }
-  return hipGetLastError();
+  return launch(a, s, read<MCA_TYPE_F32>, read<MCA_TYPE_BF16>, read<MCA_TYPE_F16>);
 }
 
 }  // namespace mca

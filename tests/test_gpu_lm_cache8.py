@@ -126,6 +126,25 @@ def test_extreme_values(lm, typ):
         assert (d <= lim)[fin[a:b]].all()
 
 
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("dim,block", [(32, 16), (128, 64), (128, 300), (64, 500)])
+def test_extreme_values_in_pages_of_every_size(lm, typ, dim, block):
+    """What is no number in some pages, heads and one of K and V alone, in pages that one wave takes, four do, and that
+    do not fit their registers; values as large as the type's in others."""
+    s = make(21, typ, [0, 7, 3, 0], [2 * block + 5, block, 3 * block, block - 1], 2, dim, block)
+    n = s["offsets"][-1].item()
+    k, v = s["k"].clone(), s["v"].clone()
+    g = torch.Generator().manual_seed(3)
+    for x, share in ((k, 0.3), (v, 0.01)):
+        at = torch.nonzero(torch.rand(n, generator=g) < share)[:, 0].cuda()
+        x[at, 0, at % dim] = torch.tensor([float("nan"), float("inf"), -float("inf")], device="cuda", dtype=x.dtype)[at % 3]
+    v[n - block // 2, 1, 3] = torch.finfo(v.dtype).max
+    k[block // 2, 1] = -0.0
+    k[block + 1, 1, :3] = torch.finfo(k.dtype).tiny
+    s["k"], s["v"] = k, v
+    check(lm, s, typ)
+
+
 def test_growth_beyond_every_kept_code(lm):
     """Kept values of 2^-60 beside new ones of 2^60: codes 0, their sign kept; NaN codes stay."""
     s = make(5, "f32", [5], [2], 1, 32, 8)

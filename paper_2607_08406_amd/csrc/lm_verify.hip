@@ -16,8 +16,8 @@
 // What bounds it: only the first step moves many bytes.  The others are chains of short
 // kernels, whose time is their launch, the spread of their workgroups and 64-bit
 // arithmetic (about 25 operations a symbol).  bf16, 32 requests of up to 9 nodes, 128000
-// symbols: rows 21 us (82 MB, 3.9 TB/s), walk 25, sums 11, draw 24, its further steps 16, 4
-// and 3: 100 us in a graph.
+// symbols: rows 21 us (82 MB, 3.9 TB/s), walk 19, sums 11, draw 23, its further steps 16, 4
+// and 3: 93 us in a graph.
 #include <algorithm>
 
 #include "device_common.hpp"
@@ -70,19 +70,18 @@ struct VerifyDev {
 };
 
 // 16 bytes at any address
-template <int TYPE>
-__device__ __forceinline__ void load_any(const char* p, float (&f)[Elem<TYPE>::kPer]) {
+__device__ __forceinline__ u32x4 any_vector(const char* p) {
   struct __attribute__((packed)) Any {
     u32x4 x;
   };
-  unpack<TYPE>(((const Any*)p)->x, f);
+  return ((const Any*)p)->x;
 }
 // symbols v .. v + kPer - 1 of a row of V; behind it -inf
 template <int TYPE>
 __device__ __forceinline__ void load_symbols(const char* row, int v, int V, float (&f)[Elem<TYPE>::kPer]) {
   constexpr int VE = Elem<TYPE>::kPer;
   if (v + VE <= V) {
-    load_any<TYPE>(row + (int64_t)v * Elem<TYPE>::kSize, f);
+    unpack<TYPE>(any_vector(row + (int64_t)v * Elem<TYPE>::kSize), f);
   } else {
 #pragma unroll
     for (int i = 0; i < VE; ++i)
@@ -282,15 +281,44 @@ __device__ __forceinline__ double left_sum(const mca_verify_drafts_args& a, int 
   // logarithms (base 2) of the factors of the exponentials
   const float fp = -__builtin_amdgcn_logf((float)s.sum[0][node]), fq = __builtin_amdgcn_logf((float)(c / s.sum[1][node]));
   double mine = 0;
-#pragma unroll 4
-  for (int v = threadIdx.x * VE; v < V; v += THREADS * VE) {
-    float x[VE], y[VE], w = 0.f;
-    load_symbols<TYPE>(zt, v, V, x);
-    load_symbols<TYPE>(zd, v, V, y);
+  auto weigh = [&](const float (&x)[VE], const float (&y)[VE]) {
+    float w = 0.f;
 #pragma unroll
     for (int e = 0; e < VE; ++e)
       w += fmaxf(__builtin_amdgcn_exp2f(fmaf(x[e] - mp, kp, fp)) - __builtin_amdgcn_exp2f(fmaf(y[e] - mq, kq, fq)), 0.f);
     mine += (double)w;
+  };
+  // All loads of a round before its sums.  A thread's last vectors are moved up to the row's
+  // end, and what was there before them (all of those that lie behind it) is left out.
+  const int v0 = (int)threadIdx.x * VE;
+  if (V < VE) {
+    float x[VE], y[VE];
+    load_symbols<TYPE>(zt, v0, V, x);
+    load_symbols<TYPE>(zd, v0, V, y);
+    if (v0 == 0) weigh(x, y);
+    return group_sum<THREADS / 64>(mine, s.red);
+  }
+#pragma unroll 1
+  for (int b = 0; b < V; b += kVUnroll * THREADS * VE) {
+    u32x4 xs[kVUnroll], ys[kVUnroll];
+#pragma unroll
+    for (int u = 0; u < kVUnroll; ++u) {
+      const int at = min(b + v0 + u * THREADS * VE, V - VE);
+      xs[u] = any_vector(zt + (int64_t)at * EL);
+      ys[u] = any_vector(zd + (int64_t)at * EL);
+    }
+#pragma unroll
+    for (int u = 0; u < kVUnroll; ++u) {
+      float x[VE], y[VE];
+      unpack<TYPE>(xs[u], x);
+      unpack<TYPE>(ys[u], y);
+      const int skip = b + v0 + u * THREADS * VE - (V - VE);
+      if (skip > 0) {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) x[e] = e < skip ? -__builtin_huge_valf() : x[e];
+      }
+      weigh(x, y);
+    }
   }
   return group_sum<THREADS / 64>(mine, s.red);
 }
@@ -529,8 +557,8 @@ __device__ __forceinline__ int last_of(int last, int* s_found) {
 
 // A request's walk over a large vocabulary, from the rows' parts.  One workgroup, as
 // whether a child is accepted decides which row is read next; a pass for S over 128000
-// symbols at one rejection takes it 8 us (in 16 waves; in 4 it took 15).  Only children
-// behind a rejected one need such a pass.
+// symbols at one rejection takes it 6 us (8 where a thread's loads waited for its sums, 15 in
+// 4 waves).  Only children behind a rejected one need such a pass.
 template <int TYPE, bool GREEDY>
 __global__ __launch_bounds__(kWalkThreads) void k_lm_verify_walk(VerifyDev d) {
   const mca_verify_drafts_args& a = d.a;

@@ -96,6 +96,16 @@ def test_many_rejections_at_a_node(lm, typ, mode, vocab):
     assert lost > 6
 
 
+@pytest.mark.parametrize("typ", TYPES)
+@pytest.mark.parametrize("vocab", [3, 5, 7, 8, 9, 15, 33, 8191, 8193, 8200, 32767, 32775, 65537])
+def test_sums_at_the_ends_of_rows(lm, typ, vocab):
+    """Vocabularies about the vectors, workgroups and rounds of the sums that rejections need."""
+    for kids in (2, 4):
+        s = make(100 + kids, typ, [kids + 1] * 6 + [2 * kids + 1] * 2, vocab, kids, "draft", noise=0.5)
+        s["accept"].uniform_(0.7, 1.0, generator=torch.Generator("cuda").manual_seed(kids))
+        check(lm, s)
+
+
 @pytest.mark.parametrize("pad", [1, 3, 8])
 @pytest.mark.parametrize("typ", ["bf16", "f32"])
 def test_rows_apart(lm, typ, pad):

@@ -7,9 +7,9 @@
 // block's tokens arrive change anything else.
 //
 // Both are bound by memory, and of few tokens by a chain of loads (offsets, the block's
-// number, its scale, the rows): bf16, 8 heads of 128, 65000 rows of 32 requests'
-// prompts are 81 us (266 MB read, 133 written, 4.9 TB/s), the values of 50000 tokens 72 us
-// (102 MB read, 205 written, 4.3 TB/s); 64 requests of 8 rows, 4 heads of 32 fp32, 5.0 and 4.7 us.
+// number, its scale, the rows): bf16, 8 heads of 128, 60500 rows of 32 requests'
+// prompts are 80 us (248 MB read, 124 written, 4.6 TB/s), the values of 51200 tokens 72 us
+// (105 MB read, 210 written, 4.4 TB/s); 64 requests of 8 rows, 4 heads of 32 fp32, 5.0 and 4.7 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -358,8 +358,8 @@ namespace {
 
 // Waves of a page and head: one while its loads in flight are all of a page's new rows, else
 // four.  (us with one and four, 8 heads, bf16: 32 requests of 8 rows of 128 5.8 and 6.5, of 24 7.8
-// and 5.9, of 40 10.2 and 6.1; the 65000 rows above in blocks of 64 101 and 80, of 32 85 and 79, of 16
-// 77 and 100, of 256 141 and 107; read back 50000 tokens of blocks of 64 73 and 72, of 32 70 and 71, of
+// and 5.9, of 40 10.2 and 6.1; the 60500 rows above in blocks of 64 101 and 80, of 32 85 and 79, of 16
+// 77 and 100, of 256 141 and 107; read back 51200 tokens of blocks of 64 73 and 72, of 32 70 and 71, of
 // 16 68 and 84; 120 of 4 heads of 32 fp32 4.7 and 6.3.)
 template <class Args>
 int waves_of(const Args& a) {

@@ -337,6 +337,16 @@ struct Rows {
   __device__ __forceinline__ void add(int h, const uint32_t (&vf)[8][VD]) {
     add_words(h, [&](int j, int d) { return vf[j][d]; });
   }
+  // the same of values that are operands already: value(e) is those of the lane's dimension e
+  template <class V>
+  __device__ __forceinline__ void add_operands(int h, V value) {
+#pragma unroll
+    for (int e = 0; e < OT; ++e) {
+      const u32x4 v = value(e);
+#pragma unroll
+      for (int t = 0; t < QT; ++t) o[t][e] = mma32<TYPE>(v, pw[t][h], o[t][e]);
+    }
+  }
   // Drafted nodes: one that some rows do not see may hold anything.  Values that
   // are not finite (bits of `odd`) are left out of the products and added for the
   // rows that see them; value(at) is node `at`'s row of V in memory.
@@ -1027,6 +1037,68 @@ __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 
         }
       }
     };
+    // V of codes in the order of its product's operand, of head_dim 128 in 16 bits: a part
+    // is a dimension's 8 tokens 4 q .. 4 q + 3 and 16 + those of half a tile, dimension 8 x + y
+    // in place 16 y + x, so that the 16 lanes of one read have neighbours.  A thread takes
+    // PER neighbouring tokens' 8 dimensions; tokens that are not there become zeros.  That
+    // saves the 64 permutations of a tile's values in each wave for 16 of each thread (16 requests
+    // of 16384, bf16, 1024 rows a key head 600 and 632 us, fp16, 64 rows 158 and 164), but not where
+    // four waves of 32 rows fill their registers: the reads then wait for each product, while
+    // permutations pass behind products (192 to 384 rows 284 and 269).
+    constexpr bool OPERAND = C8 && TYPE != MCA_TYPE_F32 && DP == 128 && (QT == 1 || NW == 8);
+    uint64_t v_there = 0;  // which tokens of the values on their way are there
+    // (a wave's threads store whole parts, so that they take all banks)
+    const int vc = tid % NCH, vx = tid / NCH / (PER == 2 ? 2 : 1);
+    const int vt = 4 * ((vx >> 3) * 8 + (vx & 1) * 4 + (vx >> 1 & 3)) + (PER == 2 ? tid / NCH % 2 * 2 : 0);
+    auto fetch_v8 = [&](const char* base, int row) {
+      if constexpr (OPERAND) {
+        v_there = __ballot(row >= 0);
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+          const uint64_t rw = (uint32_t)__shfl(max(row, 0), vt + u, 64);
+          if (!PAD || vc * CB < a.head_dim) {
+            load_codes<CB>(base + rw * (uint32_t)a.head_dim + vc * CB, cv[u]);
+          } else {
+#pragma unroll
+            for (int d = 0; d < CW; ++d) cv[u][d] = 0;
+          }
+        }
+      } else {
+        fetch8(base, row, cv);
+      }
+    };
+    auto store_v8 = [&](char* buf, int scale) {
+      if constexpr (OPERAND) {
+        static_assert(PER == 2 || PER == 4, "pairs of tokens");
+        uint32_t w[PER][4];
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+          const u32x4 x = wide_part<TYPE>(cv[u], scale_of((uint32_t)__shfl(scale, vt + u, 64)));
+#pragma unroll
+          for (int d = 0; d < 4; ++d) w[u][d] = x[d];
+        }
+        if (v_there != ~0ull) {
+#pragma unroll
+          for (int u = 0; u < PER; ++u)
+#pragma unroll
+            for (int d = 0; d < 4; ++d) w[u][d] = (v_there >> (vt + u)) & 1 ? w[u][d] : 0u;
+        }
+        const int g = vt / 4, q_ = g & 3, at = (((g >> 3) * 4 + q_) * DP + vc) * 16 + (g >> 2 & 1) * 8 + (vt & 2) * 2;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          uint32_t y[PER / 2];
+#pragma unroll
+          for (int u = 0; u < PER / 2; ++u)
+            y[u] = __builtin_amdgcn_perm(w[2 * u + 1][e >> 1], w[2 * u][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+          if constexpr (PER == 4)
+            *(u32x2*)&buf[at + e * 256] = u32x2{y[0], y[1]};
+          else
+            *(uint32_t*)&buf[at + e * 256] = y[0];
+        }
+      } else {
+        store8(buf, cv, scale);
+      }
+    };
     // what a lane reads of the first 16 rows: part i of row li is at k0 ^ 64 i, its
     // words of row 4 q + j at (v0 ^ 16 vkey(j)) + j RB; 16 rows on, the places are the same
     const int k0 = place_of(li, q), v0 = place_of(4 * q, li * CD / 4) + (li * CD * 4 & 15);
@@ -1087,12 +1159,12 @@ __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 
       // which tokens of a tile are there: of the one whose products are next, the one
       // whose scores are, and those behind it
       uint64_t t_prod = 0, t_now = __ballot(row_v >= 0), t_1 = __ballot(row_k >= 0), t_2 = 0, t_3 = 0;
-      const char *kc = (const char*)a.k_cache, *vc = (const char*)a.v_cache;
+      const char *kc = (const char*)a.k_cache, *v_cache = (const char*)a.v_cache;
       // stores tile i's keys and tile i - 1's values and requests the next ones
       auto stage = [&](int i) {
         if constexpr (C8) {
           store8(s_kv[i & 1][0], ck, k_of_k);
-          store8(s_kv[(i - 1) & 1][1], cv, v_of_v);
+          store_v8(s_kv[(i - 1) & 1][1], v_of_v);
         } else {
           store(s_kv[i & 1][0], sk);
           store(s_kv[(i - 1) & 1][1], sv);
@@ -1104,10 +1176,10 @@ __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 
           v_of_v = v_of_k;
           scales_of(blk, row_k, &k_of_k, &v_of_k);
           fetch8(kc, row_k, ck);
-          fetch8(vc, row_v, cv);
+          fetch_v8(v_cache, row_v);
         } else {
           fetch(kc, w.dbytes, row_k, sk);
-          fetch(vc, w.dbytes, row_v, sv);
+          fetch(v_cache, w.dbytes, row_v, sv);
         }
         blk = block_at(i + 2);
       };
@@ -1115,6 +1187,11 @@ __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 
         const char* V = s_kv[i & 1][1];
 #pragma unroll
         for (int half = 0; half < NH; ++half) {
+          if constexpr (OPERAND) {
+            w.add_operands(half, [&](int e) { return *(const u32x4*)&V[((half * 4 + q) * DP + e * 16 + li) * 16]; });
+            __builtin_amdgcn_sched_barrier(0);
+            continue;
+          }
           uint32_t vf[8][VD];
           values(V, half, vf);
           if ((t_prod & kAll) != kAll) w.clear(vf, (uint32_t)(t_prod >> (32 * half)));
@@ -1128,12 +1205,12 @@ __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 
         store8(s_kv[tile0 & 1][0], ck, k_of_k);
         scales_of(blk1, row_k, &k_of_k, &v_of_k);
         fetch8(kc, row_k, ck);
-        fetch8(vc, row_v, cv);
+        fetch_v8(v_cache, row_v);
       } else {
         fetch(kc, w.dbytes, row_v, sk);
         store(s_kv[tile0 & 1][0], sk);
         fetch(kc, w.dbytes, row_k, sk);
-        fetch(vc, w.dbytes, row_v, sv);
+        fetch(v_cache, w.dbytes, row_v, sv);
       }
       __syncthreads();
       if (late) {

@@ -152,6 +152,30 @@ def test_what_is_not_seen_reaches_nothing(lm, nodes):
     check(s, lm.mca_tree_attention8(**s))
 
 
+@pytest.mark.parametrize("typ", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [128, 112])
+@pytest.mark.parametrize("heads,nodes", [(2, 20), (2, 128), (4, 12), (2, 40)])
+def test_many_rows_over_what_is_not_there(lm, typ, dim, heads, nodes):
+    """The same of many rows: tiles that end inside a block of odd size, blocks outside the pool in the middle, at a
+    tile's end, at a request's, all of one."""
+    block = 19
+    s = make(31, typ, [345, 64, 128, 700, 19], [nodes, 3, nodes, nodes, 2], heads, 1, dim, block)
+    table, lens = host(s["table"]), host(s["lengths"])
+    kc, vc = host(s["k_cache"]), host(s["v_cache"])
+    seen = np.zeros(kc.shape[:3], bool)
+    for r, n in enumerate(lens):
+        for t in range(n):
+            seen[table[r, t // block], :, t % block] = True
+    kc[~seen], vc[~seen] = 0x7f, 0xff
+    table[0, 3], table[0, 345 // block], table[3, 5:9], table[4, 0] = 10 ** 6, -1, -7, kc.shape[0]
+    s.update(k_cache=codes(kc), v_cache=codes(vc), table=put(table))
+    check(s, lm.mca_tree_attention8(**s))
+    check(s, lm.mca_tree_attention8(**s, max_len=LONG))
+    vc[table[2, 1], 0, 3, 7] = 0x7f  # and a NaN that is seen
+    s["v_cache"] = codes(vc)
+    check(s, lm.mca_tree_attention8(**s, max_len=LONG))
+
+
 @pytest.mark.parametrize("nodes", [2, 70])
 def test_nan_that_is_seen(lm, nodes):
     """A NaN among a request's values makes its rows' columns NaN, one among its keys its rows; other requests' are

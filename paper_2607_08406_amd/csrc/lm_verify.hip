@@ -1004,7 +1004,7 @@ int row_splits(const mca_verify_drafts_args& a) {
 // more.  (Us, bf16, with 256, 512, 1024 and 2048 workgroups: 32 requests of trees, 128000 symbols
 // 133, 107, 100 and 105; 150 chains of 4 drafts, 32000 symbols 87, 70, 68 and 69.  With parts of 4096 symbols
 // and of 2048: one request of 128000 symbols 30.5 and 28.7, 8 of 50000 35.6 and 31.5, 32 of 32000 with four
-// children a node 111 and 116.)
+// children a node 111 and 116.  Half as many workgroups of 512 threads take 104 for 94, of 1024 122.)
 int end_cuts(const mca_verify_drafts_args& a) {
   const int64_t reqs = std::max(1, a.n_req), cuts = (a.n_vocab + kVCut - 1) / kVCut;
   return (int)std::clamp<int64_t>(std::min(cuts, (1024 + reqs - 1) / reqs), 1, kVMaxSplits);

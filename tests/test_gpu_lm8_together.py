@@ -202,3 +202,49 @@ def test_a_step_over_the_cache_of_8_bits(lm, typ, captured):
         lens.copy_(kept["got"].new_len)
         last = got[2]
     assert total > 5
+
+
+def test_two_streams_at_once(lm):
+    """Each operator on two streams, whose calls overlap, gives what it gives alone; workspaces are the calls' own."""
+    g = torch.Generator("cuda").manual_seed(2)
+    i32 = torch.int32
+    R, n, V, H, D, B, W = 24, 6, 40000, 2, 128, 16, 40
+    sets = []
+    for _ in range(2):
+        lens = torch.randint(0, B * W - n, (R,), generator=g, device="cuda").to(i32)
+        table = torch.randperm(R * W, generator=g, device="cuda").view(R, W).to(i32)
+        rand = lambda *shape: torch.randn(*shape, generator=g, device="cuda")  # noqa: E731
+        parents = torch.arange(-1, n - 1, device="cuda").repeat(R).to(i32)
+        sets.append(dict(
+            lens=lens, table=table, offsets=torch.arange(R + 1, device="cuda", dtype=i32) * n, parents=parents,
+            k=rand(R * n, H, D).bfloat16(), v=rand(R * n, H, D).bfloat16(), q=rand(R * n, 4 * H, D).bfloat16(),
+            caches=[torch.randint(0, 120, (R * W, H, B, D), generator=g, device="cuda", dtype=torch.uint8).view(torch.float8_e4m3fn)
+                    for _ in range(2)] + [torch.full((R * W, H), 122, device="cuda", dtype=torch.uint8) for _ in range(2)],
+            target=rand(R * n, V).mul_(2).bfloat16(), draft=rand(R * n, V).mul_(2).bfloat16(),
+            tokens=torch.randint(0, V, (R * n,), generator=g, device="cuda").to(i32),
+            accept=torch.rand(R * n, generator=g, device="cuda"), sample=torch.rand(R, generator=g, device="cuda")))
+
+    def calls(s):
+        caches = [c.clone() for c in s["caches"]]
+        lm.mca_cache8_append(s["k"], s["v"], *caches, s["table"], s["lens"], s["offsets"])
+        out = list(lm.mca_tree_attention8(s["q"], s["k"], s["v"], *caches, s["table"], s["lens"], s["offsets"], s["parents"], n))
+        out += lm.mca_verify_drafts(s["target"], s["draft"], s["tokens"], s["parents"], s["offsets"], s["lens"], n, s["accept"],
+                                    s["sample"])
+        top = lm.mca_token_logprobs(s["draft"], s["tokens"], 8)
+        loss = lm.mca_distill(s["target"], top.top_logprob, top.top_id, True)
+        out += [loss.loss, lm.mca_distill_grad(s["target"], top.top_logprob, top.top_id, loss.lse, loss.lse_rest, s["accept"], True)]
+        return out + [c.view(torch.uint8) for c in caches]
+
+    alone = [calls(s) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[], []]
+    for _ in range(4):
+        for i, s in enumerate(sets):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(calls(s))
+    torch.cuda.synchronize()
+    for want, runs in zip(alone, got):
+        for run in runs:
+            for a, b in zip(want, run):
+                assert torch.equal(a, b)

@@ -237,7 +237,8 @@ __global__ __launch_bounds__(kDsThreads + 64) void k_lm_distill(mca_distill_args
     u32x4 x[kDsUnroll];
 #pragma unroll
     for (int u = 0; u < kDsUnroll; ++u) x[u] = gload(vec + min(b + 64 * u + lane, v1 - 1));
-    // the teacher's symbols among these: their values become -inf
+    // the teacher's symbols among these: their values become -inf, in every lane that holds
+    // their vector (those behind the last vector hold it, too)
     const int s0 = head + b * VE;
     for (uint64_t some = __ballot(mine >= s0 && mine - s0 < 64 * kDsUnroll * VE); some != 0; some &= some - 1) {
       const int in = __builtin_amdgcn_readlane(mine, (int)__builtin_ctzll(some)) - s0, v = in / VE, word = in % VE * EL / 4;
@@ -248,7 +249,7 @@ __global__ __launch_bounds__(kDsThreads + 64) void k_lm_distill(mca_distill_args
       for (int u = 0; u < kDsUnroll; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const bool this_one = v == 64 * u + lane && i == word;
+          const bool this_one = v == min(64 * u + lane, v1 - 1 - b) && i == word;
           x[u][i] = this_one ? (x[u][i] & keep) | (low << shift) : x[u][i];
         }
     }
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(kDsThreads + 64) void k_lm_distill(mca_distill_args
 #pragma unroll
       for (int i = 0; i < VE; ++i) top = fmaxf(top, f[i]);
     }
-    // (vectors behind the last are read twice: they do not raise the maximum)
+    // (lanes behind the last vector hold that one: its maximum is theirs)
     if (top > a.m) a.move(top, k2);
     float sum[kDsUnroll];
 #pragma unroll

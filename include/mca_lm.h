@@ -346,8 +346,8 @@ int mca_distill(const mca_distill_args* args, void* hip_stream);
  *   grad_v = grad_loss scale (Q s_v - sum_{j: id_j = v} q_j),  Q = sum_j q_j + q_r,
  * and of symbols that are none of the teacher's with rest 1
  *   grad_v = grad_loss s_v (Q - q_r / s_r).
- * A row of lse -inf has gradient 0, one whose loss is NaN a NaN.  (grad_loss 0 gives 0
- * for every finite loss.)  grad has the logits' type, rows grad_row apart, and may be
+ * A row whose loss is NaN has a gradient of NaN, another one of lse -inf a gradient of 0.
+ * (grad_loss 0 gives 0 for every finite loss.)  grad has the logits' type, rows grad_row apart, and may be
  * the logits themselves (same address and stride). */
 typedef struct mca_distill_grad_args {
   int32_t dtype, n_top, rest;

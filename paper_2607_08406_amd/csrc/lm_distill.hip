@@ -345,7 +345,6 @@ __device__ __forceinline__ RowGrad row_grad(const mca_distill_grad_args& p, int6
   const bool rest = p.rest != 0;
   const Logs lp = logs_of(p, e);
   r.lse = r.lse_other = p.lse[t];
-  r.zero = !lp.any || r.lse == -__builtin_huge_valf();
   const float lr = rest ? p.lse_rest[t] : 0.f;
   const bool nothing = rest && lr == -__builtin_huge_valf();  // then the others' exponentials are 0
   // the entries' probabilities, and in lane 63 the student's of the others
@@ -353,13 +352,15 @@ __device__ __forceinline__ RowGrad row_grad(const mca_distill_grad_args& p, int6
   double sum = lane < 32 ? q : 0.0;
   for (int d = 1; d < p.n_top; d <<= 1) sum += __shfl_xor(sum, d, 64);
   sum = lane_of(sum, 0);
+  const bool undefined = sum != sum || r.lse != r.lse;  // so is the loss
+  r.zero = !lp.any || (r.lse == -__builtin_huge_valf() && !undefined);
   const double left = rest ? fmax(1.0 - sum, 0.0) : 0.0;
   // (without rest the entries' sum to 1, if any has some)
   const double total = rest ? (sum != sum ? sum : sum + left) : (lp.none ? 0.0 : (sum != sum ? sum : 1.0));
   r.known = r.other = (float)(g * total);
   if (rest) {
     r.lse_other = nothing ? 0.f : lr;
-    r.other = nothing ? 0.f : (float)(g * (total * lane_of(q, 63) - left));
+    r.other = nothing ? (undefined ? __builtin_nanf("") : 0.f) : (float)(g * (total * lane_of(q, 63) - left));
   }
   *off = (float)(lp.none ? 0.0 : g * (rest ? q : q / sum));
   return r;

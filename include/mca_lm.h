@@ -239,8 +239,9 @@ int mca_tree_attention8(const mca_tree_attention8_args* args, void* hip_stream);
  * has children) has no softmax (NaN, +inf, nothing but -inf),
  * the path ends and token is -1; so it is for requests without nodes, of more than
  * max_nodes or of offsets out of range, whose new_len is lengths[r].
- * Sums are held in 64 bits, of exponentials of 32 where a child is tried and of 64 where
- * a token is drawn (there c is a sum of such ones, too). */
+ * Sums are held in 64 bits, of exponentials of 64 where a token is drawn (there c is a sum of
+ * such ones, too), and where a child is tried of 32: each off by (1 + |exponent|) 2^-22 at
+ * most, and up to 8 neighbours added before they go into a sum. */
 typedef struct mca_verify_drafts_args {
   int32_t dtype, n_req, max_nodes, greedy;
   int64_t n_rows, n_vocab, target_row, draft_row;

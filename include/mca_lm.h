@@ -156,7 +156,8 @@ int mca_tree_attention(const mca_tree_attention_args* args, void* hip_stream);
  * lie in the block, not below the one it has; where it grows, their codes are
  * rounded to the new one, which changes only those that become less than 2^-6.
  * Values are rounded to nearest, ties to even; those whose code would stand for
- * more than the source type holds (from 248 times 2^120, of fp16 2^8) become 240.
+ * more than the source type holds (from 248 times 2^120, of fp16 2^8) get the largest
+ * code that does not: 240 at that scale, and at the larger ones that blocks with tokens kept may have less.
  * Infinities and NaN become the code 0x7f and do not count for the scale.  A row
  * outside [0, n_src) counts as zeros.  Blocks outside [0, n_blocks), positions
  * behind max_blocks, and requests of negative lengths or of offsets out of range are

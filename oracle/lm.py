@@ -203,7 +203,8 @@ def cache8_append(k, v, k_cache, v_cache, k_scale, v_scale, table, lengths, offs
                         if e > before:
                             kept = e4m3(e4m3_value(cache[blk, h, :keep]) * 2.0 ** (before - e))
                             cache[blk, h, :keep] = np.where(np.isnan(kept), cache[blk, h, :keep], e4m3_code(kept))
-                    most = 240.0 if e >= CLAMPED_EXP[typ] else 448.0
+                    t = 2.0 ** (CLAMPED_EXP[typ] + 8 - e)  # a code of this is past the type's largest value
+                    most = max(0.0, t - max(t / 16, 2.0 ** -9)) if e >= CLAMPED_EXP[typ] else 448.0
                     y = np.clip(np.where(fin, new, 0.0) * 2.0 ** -e, -most, most)
                     code = e4m3_code(e4m3(np.where(fin, y, np.nan)))
                     for i, c in zip(those, code):

@@ -38,6 +38,13 @@ struct Scale {
   static constexpr int kLeast = TYPE == MCA_TYPE_F16 ? -15 : -100, kFull = TYPE == MCA_TYPE_F16 ? 8 : 120;
 };
 
+// The largest code's value that, times 2^e, the type holds: the one below 2^(kFull + 8 - e).
+template <int TYPE>
+__device__ __forceinline__ float most_of(int e) {
+  const int t = Scale<TYPE>::kFull + 8 - e;
+  return t > 8 ? 448.f : fmaxf(__builtin_ldexpf(1.f, t) - __builtin_ldexpf(1.f, max(t - 4, -9)), 0.f);
+}
+
 // The pages of all requests laid end to end with room to spare: request r's begin at
 // offsets[r] / B + 2 r, which leaves each at least its (tokens / B) + 2, and `items` of
 // the whole call can be had from what the host knows.  A wave looks 64 requests up
@@ -270,7 +277,7 @@ __global__ __launch_bounds__(kC8Threads<W>) void k_lm_append8(mca_cache8_append_
   uint8_t* kc = a.k_cache + at * a.block_size * a.head_dim;
   uint8_t* vc = a.v_cache + at * a.block_size * a.head_dim;
   auto write = [&](auto plain) {
-    const float most_k = ek >= S::kFull ? 240.f : 448.f, most_v = ev >= S::kFull ? 240.f : 448.f;
+    const float most_k = most_of<TYPE>(ek), most_v = most_of<TYPE>(ev);
     const float by_k = __builtin_ldexpf(1.f, -ek), by_v = __builtin_ldexpf(1.f, -ev);
     for (int c = last; c >= 0; c -= T * kC8Loads) {
       if (c != last) load(c);

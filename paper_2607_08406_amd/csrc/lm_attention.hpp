@@ -603,10 +603,10 @@ __device__ __forceinline__ bool share_begin(const AttnDev& p, int (&s_wave)[NW],
 // memory still hides: 32 single tokens behind 8192 to 32768, 8 key heads of 128, 4 rows a
 // head, bf16 (1.33 GB): 250 us and 10 of joining, 5.3 TB/s; the drafts of 8 8.1 us.
 
-// Waves of a SIMD that its registers are for, of 8-bit caches; of shared work few enough
-// that nothing of the loop around the items goes to scratch memory.
+// Waves of a SIMD that its registers are for, of 8-bit caches; of shared work (head_dim above
+// 64) few enough that nothing of the loop around the items goes to scratch memory.
 constexpr int resident8(int type, int dp, bool share) {
-  if (share) return dp <= 64 ? (type == MCA_TYPE_F32 ? 2 : 3) : (dp <= 128 ? 2 : 1);
+  if (share) return dp <= 128 ? 2 : 1;
   return dp <= 64 ? (type == MCA_TYPE_F32 ? 3 : 4) : (dp <= 128 ? (type == MCA_TYPE_F32 ? 2 : 3) : 1);
 }
 template <int TYPE, int DP, bool PAD, bool C8, bool SHARE = false>
@@ -1327,11 +1327,11 @@ __global__ __launch_bounds__(256) void k_lm_attn_join(AttnDev p) {
 // rows, which are cut in the same places, 4 at a time: their weights are made in
 // LDS, then its NW waves take parts in turn and are added there.  head_dim is at
 // most 64 NI.
-constexpr int kMaxSharers = 512, kMaxSharers8 = 1024;  // workgroups, and those of the narrow kernel
-template <int TYPE, int NI, int NW, int SHARERS>
+constexpr int kMaxSharers = 512;  // workgroups: two a compute unit
+template <int TYPE, int NI, int NW>
 __global__ __launch_bounds__(64 * NW) void k_lm_attn_join_shared(AttnDev p, int TP, int fours) {
   const mca_tree_attention_args& a = p.a;
-  __shared__ float s_w[4][SHARERS];
+  __shared__ float s_w[4][kMaxSharers];
   __shared__ float s_acc[NW][4 * 64 * NI];
   const int groups = p.rows / (4 * fours), tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int tile = blockIdx.x / groups, rt = tile % p.row_tiles, rh = tile / p.row_tiles;
@@ -1484,7 +1484,7 @@ void launch_pad(const AttnDev& p, dim3 grid, hipStream_t s) {
   constexpr bool kBig = DP > (TYPE == MCA_TYPE_F32 ? 64 : 128);             // big_rows()
   constexpr bool kEight = TYPE == MCA_TYPE_F32 ? DP == 128 : DP >= 128;     // wide_waves() may be 8
   if (!is_wide<C8>(p.a)) {
-    if constexpr (C8)
+    if constexpr (C8 && DP > 64)
       if (p.sharers > 0) {
         hipLaunchKernelGGL((k_lm_attn<TYPE, DP, PAD, C8, true>), grid, dim3(kAttnThreads), 0, s, p);
         return;
@@ -1517,12 +1517,11 @@ void launch_dim(const AttnDev& p, dim3 grid, hipStream_t s) {
 // 8192, 128 rows, head_dim 128, 512 workgroups, 58 and 54).
 template <int TYPE, int NI, bool C8>
 void launch_join(const AttnDev& p, dim3 groups, int fours, hipStream_t s) {
-  constexpr int SHARERS = C8 ? kMaxSharers8 : kMaxSharers;
   const int tokens = is_wide<C8>(p.a) ? tile_tokens(p.a) : kAttnWaves * kTilePos;
   if (groups.x <= kCUs)
-    hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 16, SHARERS>), groups, dim3(1024), 0, s, p, tokens, fours);
+    hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 16>), groups, dim3(1024), 0, s, p, tokens, fours);
   else
-    hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 4, SHARERS>), groups, dim3(256), 0, s, p, tokens, fours);
+    hipLaunchKernelGGL((k_lm_attn_join_shared<TYPE, NI, 4>), groups, dim3(256), 0, s, p, tokens, fours);
 }
 template <int TYPE, bool C8>
 void launch_type(const AttnDev& p, dim3 grid, hipStream_t s) {
@@ -1588,6 +1587,7 @@ AttnPlan attention_plan(const mca_tree_attention_args& a) {
     // 1000 131 and 108.
     const bool big = a.dtype == MCA_TYPE_F32 && a.head_dim > 128;
     const int64_t units = wgs * ((a.max_len + kAttnWaves * kTilePos - 1) / (kAttnWaves * kTilePos) + 1);
+    static_assert(2 * kCUs <= kMaxSharers, "shared work's weights in LDS");
     const int resident = kCUs * resident8(a.dtype, a.head_dim, true);
     if ((big || a.max_len >= 1 << 14) && units >= 8 * resident && units < (1 << 30)) {
       p.chunk = a.max_len;

@@ -91,21 +91,6 @@ __device__ __forceinline__ bool page_of(const Args& a, const int32_t* before, in
   return true;
 }
 
-template <int TYPE>
-__device__ __forceinline__ void widen(u32x4 x, float (&f)[TYPE == MCA_TYPE_F32 ? 4 : 8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (TYPE == MCA_TYPE_F32) {
-      f[i] = __uint_as_float(x[i]);
-    } else if constexpr (TYPE == MCA_TYPE_BF16) {
-      f[2 * i] = __uint_as_float(x[i] << 16);
-      f[2 * i + 1] = __uint_as_float(x[i] & 0xffff0000u);
-    } else {
-      f[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)x[i]);
-      f[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(x[i] >> 16));
-    }
-  }
-}
 __device__ __forceinline__ bool finite_bits(uint32_t b) { return (b & 0x7f800000u) != 0x7f800000u; }
 // four codes, rounded to nearest, of values times 2^-e, none above `most`
 __device__ __forceinline__ uint32_t codes_of(const float* f, int e, float most) {
@@ -244,7 +229,7 @@ __global__ __launch_bounds__(kC8Threads<W>) void k_lm_append8(mca_cache8_append_
     top_k = top_v = 0;
     auto look = [&](u32x4 x, uint32_t* top) {
       float f[VE];
-      widen<TYPE>(x, f);
+      unpack<TYPE>(x, f);
 #pragma unroll
       for (int i = 0; i < VE; ++i) {
         const uint32_t b = __float_as_uint(f[i]) & 0x7fffffffu;
@@ -288,7 +273,7 @@ __global__ __launch_bounds__(kC8Threads<W>) void k_lm_append8(mca_cache8_append_
         const int64_t to = (int64_t)(pg.from - pg.start) * a.head_dim + (int64_t)e * VE;
         auto put = [&](u32x4 x, uint8_t* cache, int ex, float most, float by) {
           float f[VE];
-          widen<TYPE>(x, f);
+          unpack<TYPE>(x, f);
           uint32_t w[VE / 4];
 #pragma unroll
           for (int i = 0; i < VE / 4; ++i) w[i] = plain ? codes_of(f + 4 * i, by) : codes_of(f + 4 * i, ex, most);

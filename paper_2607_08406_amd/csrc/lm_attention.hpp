@@ -567,6 +567,7 @@ __device__ __forceinline__ bool share_begin(const AttnDev& p, int (&s_wave)[NW],
   }
   // workgroups on one XCD (every eighth) take neighbouring units
   const int g = (int)(blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8), per = Share::per(p, all);
+  // g per < sharers (all / sharers + 1) + the least units of all: below 2^31
   const int u0 = g * per, u1 = min(all, u0 + per);
   for (int x = tid * some; x < (tid + 1) * some && x < n_req; ++x) {
     const int u = Share::units(p, x, TP);
@@ -887,50 +888,18 @@ __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 
   __shared__ int s_wave[NW];
   // where the workgroup stands, in LDS so that it takes no registers beside a tile's:
   // its next and last unit, its request and the units before that, its next place
-  __shared__ int s_unit, s_end, s_before, s_req, s_part;
+  __shared__ int s_unit, s_end, s_begin[2], s_part;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   int rt = 0, h = 0, r = 0, part = 0;
   if (p.sharers == 0) {
     if (!place(p, &rt, &h, &r, &part)) return;
   } else {
-    // each thread's requests, then the sums of those before them
-    const int some = (a.n_req + THREADS - 1) / THREADS;
-    int mine = 0;
-    for (int x = tid * some; x < (tid + 1) * some && x < a.n_req; ++x) mine += Share::units(p, x, TP);
-    int run = mine;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int up = __shfl_up(run, d, 64);
-      if (lane >= d) run += up;
-    }
-    if (lane == 63) s_wave[wave] = run;
-    __syncthreads();
-    int all = 0, pre = run - mine;
-#pragma unroll
-    for (int x = 0; x < NW; ++x) {
-      if (x < wave) pre += s_wave[x];
-      all += s_wave[x];
-    }
-    // workgroups on one XCD (every eighth) take neighbouring units
-    const int g = (int)(blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8);
-    const int per = Share::per(p, all);
-    // g per < sharers (all / sharers + 1) + the least units of all: below 2^31
-    const int unit = g * per, end = min(all, unit + per);
-    for (int x = tid * some; x < (tid + 1) * some && x < a.n_req; ++x) {
-      const int u = Share::units(p, x, TP);
-      if (blockIdx.x == 0) p.first_unit[x] = pre;
-      if (unit >= pre && unit < pre + u) {
-        s_req = x;
-        s_before = pre;
-      }
-      pre += u;
-    }
-    if (blockIdx.x == 0 && tid == 0) p.first_unit[a.n_req] = all;
-    if (unit >= end) return;
+    int unit, end;
+    if (!share_begin<TP, NW>(p, s_wave, s_begin, &unit, &end, &part)) return;
     if (tid == 0) {
       s_unit = unit;
       s_end = end;
-      s_part = 2 * g;
+      s_part = part;
     }
     __syncthreads();
   }
@@ -944,10 +913,10 @@ __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 
     const mca_tree_attention_args& a = p.a;
     int first, n, tile0 = 0, tile1 = 0;
     if (p.sharers > 0) {
-      int before = __builtin_amdgcn_readfirstlane(s_before);
+      int before = __builtin_amdgcn_readfirstlane(s_begin[1]);
       const int unit = __builtin_amdgcn_readfirstlane(s_unit), end = __builtin_amdgcn_readfirstlane(s_end);
       part = __builtin_amdgcn_readfirstlane(s_part);
-      r = __builtin_amdgcn_readfirstlane(s_req);
+      r = __builtin_amdgcn_readfirstlane(s_begin[0]);
       if (unit >= end) return;
       for (int units = Share::units(p, r, TP); unit >= before + units; units = Share::units(p, r, TP)) {
         before += units;
@@ -963,8 +932,8 @@ __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 
       __syncthreads();
       if (tid == 0) {
         s_unit = unit + (tile1 - tile0);
-        s_before = before;
-        s_req = r;
+        s_begin[0] = r;
+        s_begin[1] = before;
         s_part = part | 1;  // a workgroup's later items are its last, if they are cut
       }
     } else if (!rows_of(a, r, &first, &n)) {

@@ -105,7 +105,8 @@ __device__ __forceinline__ void unpack(u32x4 x, float (&f)[Elem<TYPE>::kPer]) {
 
 // Exponentials and logarithms of 64 bits (the library's are made for all numbers).
 // exp(x) of N numbers of at most 700, to 2^-47: 2^n times the series of exp in the rest,
-// which is at most ln 2 / 2, to its 11th power.  Results below 2^-1021 are 0, NaN stays.
+// which is at most ln 2 / 2, to its 11th power.  For x below -707 it is 0
+// (results below 2^-1020), NaN stays.
 // n comes from the last bits of x / ln 2 + 1.5 2^52 and goes into the exponent as bits:
 // conversions, roundings and ldexp of 64 bits take four times as long as a sum.  The steps
 // of several go side by side: one by one, each would wait for the one before.

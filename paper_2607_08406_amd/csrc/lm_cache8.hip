@@ -352,7 +352,11 @@ namespace {
 // four.  (us with one and four, 8 heads, bf16: 32 requests of 8 rows of 128 5.8 and 6.5, of 24 7.8
 // and 5.9, of 40 10.2 and 6.1; the 60500 rows above in blocks of 64 101 and 80, of 32 85 and 79, of 16
 // 77 and 100, of 256 141 and 107; read back 51200 tokens of blocks of 64 73 and 72, of 32 70 and 71, of
-// 16 68 and 84; 120 of 4 heads of 32 fp32 4.7 and 6.3.)
+// 16 68 and 84; 120 of 4 heads of 32 fp32 4.7 and 6.3.)  The host knows only how many rows a
+// request has on average.  (The same of mixed calls, appended: one prompt of 3000 among 255 single
+// tokens, blocks of 16 10.3 and 17.5, of 64 14.2 and 14.9, of 256 43 and 15, where the rule takes the slower;
+// among 30 of 8 rows 7.2 and 10.2, 7.7 and 7.6, 13.5 both.  Rows behind the last request count as rows: 64 of 8
+// and 60000 such, blocks of 16, 12.8 and 34.8, of 64 12.2 both.)
 template <class Args>
 int waves_of(const Args& a) {
   const int64_t tokens = std::min<int64_t>(a.block_size, (a.n + a.n_req - 1) / a.n_req);

@@ -349,8 +349,9 @@ int mca_distill(const mca_distill_args* args, void* hip_stream);
  * and of symbols that are none of the teacher's with rest 1
  *   grad_v = grad_loss s_v (Q - q_r / s_r).
  * A row whose loss is NaN has a gradient of NaN, another one of lse -inf a gradient of 0.
- * (grad_loss 0 gives 0 for every finite loss.)  grad has the logits' type, rows grad_row apart, and may be
- * the logits themselves (same address and stride). */
+ * (grad_loss 0 gives 0 for every finite loss.)  s_v is exp(scale z_v - lse) and off by
+ * |lse| 2^-24 of itself, as lse is rounded to 32 bits.  grad has the logits' type, rows
+ * grad_row apart, and may be the logits themselves (same address and stride). */
 typedef struct mca_distill_grad_args {
   int32_t dtype, n_top, rest;
   float scale;

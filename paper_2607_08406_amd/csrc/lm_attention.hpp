@@ -1010,10 +1010,10 @@ __global__ __launch_bounds__(64 * NW, DP * (TYPE == MCA_TYPE_F32 ? 2 : 1) > 256 
     // is a dimension's 8 tokens 4 q .. 4 q + 3 and 16 + those of half a tile, dimension 8 x + y
     // in place 16 y + x, so that the 16 lanes of one read have neighbours.  A thread takes
     // PER neighbouring tokens' 8 dimensions; tokens that are not there become zeros.  That
-    // saves the 64 permutations of a tile's values in each wave for 16 of each thread (16 requests
-    // of 16384, bf16, 1024 rows a key head 600 and 632 us, fp16, 64 rows 158 and 164), but not where
+    // saves the 64 permutations of a tile's values in each wave for 16 of each thread (16 requests of up
+    // to 16384, bf16, 1024 rows a key head 575 and 622 us, fp16, 64 rows 90 and 92), but not where
     // four waves of 32 rows fill their registers: the reads then wait for each product, while
-    // permutations pass behind products (192 to 384 rows 284 and 269).
+    // permutations pass behind products (192 to 384 rows 283 and 269).
     constexpr bool OPERAND = C8 && TYPE != MCA_TYPE_F32 && DP == 128 && (QT == 1 || NW == 8);
     uint64_t v_there = 0;  // which tokens of the values on their way are there
     // (a wave's threads store whole parts, so that they take all banks)
